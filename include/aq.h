@@ -46,7 +46,7 @@ typedef enum {
     AQ_ERR_CUDA = 4,          /* a CUDA runtime call failed (see aq_last_cuda_error) */
     AQ_ERR_TIMEOUT = 5,       /* a bounded device-side wait ran out */
     AQ_ERR_ARCH = 6,          /* current device is not sm_100 */
-    AQ_ERR_RANGE = 7          /* non-finite weight, or a block's scale/min overflows binary16 */
+    AQ_ERR_RANGE = 7          /* non-finite weight, or a block's scale/min overflows binary16; a step's device arrays that do not fit its cache */
 } aq_status_t;
 
 typedef enum { AQ_F16 = 0, AQ_BF16 = 1, AQ_F32 = 2 } aq_dtype_t;
@@ -175,6 +175,140 @@ aq_status_t aq_kv_append(void* k_cache_dev, void* v_cache_dev, const void* k_dev
 aq_status_t aq_attn_decode(const void* q_dev, const void* k_cache_dev, const void* v_cache_dev, void* out_dev, int M, int n_heads,
                            int n_kv_heads, int head_dim, int64_t L, int64_t L_max, float scale, aq_dtype_t dtype,
                            aq_dtype_t out_dtype, void* scratch_dev, size_t scratch_bytes, aq_stream_t stream);
+
+/*
+ * Serving a batch of requests from a paged key/value cache held in 8 bits: the step's plan, rotary positions of its rows, the
+ * append that quantises and the attention.  (No counterpart in the paper, whose runtime serves one request; these stand beside
+ * aq_rope, aq_kv_append and aq_attn_decode.)
+ *
+ * The cache of a layer (aq_kv8_cache_t): codes, signed bytes [n_pages][n_kv_heads][page][head_dim] for keys and for values, and
+ * one float32 scale per 32 positions of a page and head, [n_pages][n_kv_heads][page / 32]; a value is code * scale.  page: 32, 64,
+ * ... 1024; head_dim: 64, 128 or 256; 1 <= n_kv_heads <= 256.  A page can be used before anything was written to it: what lies
+ * behind a request's length is never used.
+ *
+ * A step (aq_kv8_batch_t, the same for all layers): n_seqs (1 .. AQ_KV8_MAX_SEQS) requests.  Request b has lens_dev[b] cached
+ * positions, those of the step's new tokens included, in pages table_dev[b][0], [1], ... (table_width entries per request, those past
+ * its length not read; 1 <= table_width <= 2^20, table_width * page <= 2^30).  The step's arrays have n_rows rows (1 .. AQ_MAX_M); rows
+ * row_start_dev[b] .. row_start_dev[b + 1] - 1 are request b's new tokens, its last positions in order; rows from
+ * row_start_dev[n_seqs] on are nobody's and left as they are.  row_start_dev NULL: n_rows / n_seqs rows each (n_rows % n_seqs == 0).
+ * Two requests may share pages that neither writes to.  The descriptors are read during the call; the arrays they name are read by its stream
+ * work, so a captured call follows new lengths, tables and rows.
+ *
+ * What these device arrays say cannot be checked on the host.  A page outside the pool, or a length that does not fit the table,
+ * is not followed: such positions count as masked (append: are not written), and the next aq_check on that device returns
+ * AQ_ERR_RANGE.
+ */
+#define AQ_KV8_BLOCK 32
+#define AQ_KV8_MAX_SEQS 1024
+#define AQ_KV8_SCRATCH_BYTES ((size_t)1 << 23)
+
+typedef struct {
+    void* k_dev;              /* DEVICE, signed bytes, 16-byte aligned */
+    void* v_dev;
+    float* k_scale_dev;       /* DEVICE, float32 */
+    float* v_scale_dev;
+    int64_t n_pages;          /* 1 .. 2^31 - 1 */
+    int32_t page;             /* positions per page */
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t pad_;
+} aq_kv8_cache_t;
+
+typedef struct {
+    const int32_t* lens_dev;        /* DEVICE [n_seqs] */
+    const int32_t* row_start_dev;   /* DEVICE [n_seqs + 1], or NULL */
+    const int32_t* table_dev;       /* DEVICE [n_seqs][table_width] */
+    int64_t table_width;
+    int32_t n_seqs;
+    int32_t pad_;
+} aq_kv8_batch_t;
+
+/*
+ * aq_kv8_plan -- a step's lengths, tables and row maps from the requests' lengths, on the device.
+ *   lens_dev [n_seqs]    : cached lengths before the step
+ *   new_dev [n_seqs]     : new tokens of each request (0: it rests), or -1: it has ended and its pages are free again
+ *   table_dev            : the entries for the pages that a growing request comes to need are written, others left
+ *   free_dev [free_cap], n_free_dev : the free pages, a stack; taken from its end, given back to its end (requests in order, a
+ *                          request's pages in order; giving back comes first)
+ *   lens_out_dev [n_seqs], n_free_out_dev : lengths and free pages after the step (0 for an ended request; may be lens_dev and n_free_dev)
+ *   row_start_dev [n_seqs + 1], pos_dev [n_rows] : first row of each request, and of each row its position (-1: nobody's row)
+ * page and table_width as above; 1 <= n_rows <= 2^20, 0 <= free_cap < 2^31.
+ * All or nothing: where the free pages, free_cap, table_width or n_rows do not suffice, or a length is negative, lengths, tables and free pages
+ * stay as they were, the step has no rows (row_start 0, pos -1), and aq_check returns AQ_ERR_RANGE.
+ */
+aq_status_t aq_kv8_plan(const int32_t* lens_dev, const int32_t* new_dev, int n_seqs, int page, int32_t* table_dev, int64_t table_width,
+                        int32_t* free_dev, int64_t free_cap, const int32_t* n_free_dev, int32_t* lens_out_dev, int32_t* n_free_out_dev,
+                        int32_t* row_start_dev, int32_t* pos_dev, int64_t n_rows, aq_stream_t stream);
+
+/*
+ * aq_kv8_append -- the step's new keys and values into the cache, quantised.
+ *   k_dev, v_dev : DEVICE, rows of [n_kv_heads][head_dim] of `dtype` (AQ_F16 / AQ_BF16), 16-byte aligned, `row_stride` elements (a
+ *                  multiple of 8, at least n_kv_heads * head_dim) from one row to the next
+ * For each block of 32 positions and head that the step brings rows to, with m the largest magnitude among them, s' the block's scale
+ * (0 where its first position is among them), all in binary32, one rounding per operation:
+ *   need = up11(m / 127);   s = need <= s' ? s' : max(need, up11(1.25 s'));   code = rint(x / s)   (ties to even; 0 where s = 0)
+ * up11(y): the next number of 11 significant bits not below y.  Where s > s' the block's older positions are put on the new scale,
+ * code = rint(code * s' / s).  A value is off by at most s / 2 when it is written, and by less than 2.5 s however often its block's
+ * scale grows.  A NaN or an infinity makes the scale NaN: the block reads as NaN until its first position is written again.
+ * A page that is written to must belong to one request alone.
+ */
+aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* k_dev, const void* v_dev, int64_t row_stride,
+                          int64_t n_rows, aq_dtype_t dtype, aq_stream_t stream);
+
+/*
+ * aq_kv8_attn -- out[t][h] = softmax_p(scale * q[t][h] . K[p]) V[p] over the cached positions p of row t's request up to its own;
+ * query head h reads key/value head h / (n_heads / n_kv_heads).  A row that sees no position is 0.
+ *   q_dev   : DEVICE, rows of [n_heads][head_dim] of `dtype` (AQ_F16 / AQ_BF16), 16-byte aligned, q_stride elements (a multiple of 8) apart
+ *   out_dev : DEVICE, rows of [n_heads][head_dim] of out_dtype (any of the three), 16-byte aligned, out_stride elements (a multiple of 8) apart
+ *   scale   : <= 0 means 1 / sqrt(head_dim)
+ *   scratch_dev : DEVICE, 256-byte aligned, AQ_KV8_SCRATCH_BYTES, ZERO before its first use; a call leaves it as the next one wants it.
+ *             Calls that may overlap in time (streams, captured graphs) need scratch of their own.
+ * Built for decode (a few new tokens per request against long contexts); more rows per request are right but re-read the cache
+ * for every 8 (head_dim 256) or 16 of a head's query rows.  Scores and sums are binary32; the weights enter the second product rounded to
+ * binary16, those under 2^-40 of a row's largest as 0, and are summed as rounded: against the exact result for the cached values an output
+ * is off by at most about 2^-10 sum_p softmax_p |V[p]|, 2^-18 of what the sum would be with every |V[p]| at its block's largest, and its own
+ * rounding.  A query row with a NaN or an infinity gives NaN.
+ */
+aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* q_dev, int64_t q_stride, void* out_dev,
+                        int64_t out_stride, int64_t n_rows, int n_heads, float scale, aq_dtype_t dtype, aq_dtype_t out_dtype, void* scratch_dev,
+                        size_t scratch_bytes, aq_stream_t stream);
+
+/*
+ * aq_rope_setup (HOST only) -- the frequencies of a rotary embedding: f_i = theta^(-2 i / rot_dim) for pair i of the first rot_dim
+ * (even, 2 .. 256) dims of a head, in one of the forms for contexts longer than the trained one:
+ *   AQ_ROPE_NONE    f_i as it is                AQ_ROPE_LINEAR  f_i / factor
+ *   AQ_ROPE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in theta's place (rot_dim = 2: as it is)
+ *   AQ_ROPE_PARTS   r = trained * f_i / (2 pi) rotations over the trained length: f_i for r >= high, f_i / factor for r <= low, in between
+ *                   mixed in proportion; low, high 0: 1 and 32
+ * magnitude: what rotated values are multiplied by; 0: 0.1 ln(factor) + 1 for AQ_ROPE_PARTS, else 1.
+ *   layout: AQ_ROPE_HALF pairs (i, i + rot_dim / 2), AQ_ROPE_PAIRS pairs (2 i, 2 i + 1).  theta > 1, factor >= 1, trained >= 1 (AQ_ROPE_PARTS).
+ */
+#define AQ_ROPE_MAX_PAIRS 128
+typedef enum { AQ_ROPE_HALF = 0, AQ_ROPE_PAIRS = 1 } aq_rope_layout_t;
+typedef enum { AQ_ROPE_NONE = 0, AQ_ROPE_LINEAR = 1, AQ_ROPE_BASE = 2, AQ_ROPE_PARTS = 3 } aq_rope_scaling_t;
+typedef struct {
+    double turns[AQ_ROPE_MAX_PAIRS];   /* f_i / (2 pi) */
+    float magnitude;
+    int32_t rot_dim;
+    int32_t layout;
+    int32_t pad_;
+} aq_rope_t;
+aq_status_t aq_rope_setup(int rot_dim, int layout, double theta, int scaling, double factor, double trained, double low, double high,
+                          double magnitude, aq_rope_t* out);
+
+/*
+ * aq_rope_rows -- out[t][h] = x[t][h] with pair i of its first rot_dim dims rotated by pos[t] * f_i and multiplied by the magnitude, (a, b) ->
+ * (a cos - b sin, b cos + a sin), the other dims as they are; angles in binary64, the rotation in binary32.
+ *   rope   : HOST, from aq_rope_setup (rot_dim <= head_dim), read during the call
+ *   x_dev  : DEVICE, n_rows rows of [n_heads][head_dim] of `dtype` (any of the three), x_stride elements apart
+ *   out_dev: DEVICE, likewise of out_dtype (= dtype, or a half type for AQ_F32 input), out_stride apart; may be x_dev itself with the same
+ *            type and stride (in place), else no element of the one may be one of the other
+ *   pos_dev: DEVICE int32 [n_rows]; rows with a negative position are left as they are
+ * head_dim >= 2; n_rows * n_heads < 2^31; element alignment suffices (16-byte aligned rows with multiples of 8 or 16 elements run eight at a time).
+ * Queries and keys of a fused projection rotate in one call: they are neighbouring heads of a row.
+ */
+aq_status_t aq_rope_rows(const aq_rope_t* rope, const void* x_dev, aq_dtype_t dtype, int64_t x_stride, void* out_dev, aq_dtype_t out_dtype,
+                         int64_t out_stride, int64_t n_rows, int n_heads, int head_dim, const int32_t* pos_dev, aq_stream_t stream);
 
 /*
  * aq_pack_sb / aq_import_sb / aq_export_sb -- the two-level (super-block) form of the format (Section 3, "Weight
@@ -405,6 +539,8 @@ size_t aq_stack_input_offset(const aq_stack_t* prog, int M, int op);
  * library gave up on a bounded device-side wait since the last aq_check
  * (AQ_ERR_TIMEOUT; the record is cleared) or the stream saw a CUDA error
  * (AQ_ERR_CUDA).  Outputs of a call that timed out are undefined.
+ * AQ_ERR_RANGE: an aq_kv8 call met pages, lengths or row counts in its device
+ * arrays that it could not follow (likewise cleared).
  */
 aq_status_t aq_check(aq_stream_t stream);
 

@@ -24,10 +24,14 @@ AQ_F16, AQ_BF16, AQ_F32 = 0, 1, 2
 AQ_IN_PLAIN, AQ_IN_RMSNORM, AQ_IN_SILU_MUL = 0, 1, 2
 AQ_OUT_STORE, AQ_OUT_ADD = 0, 1
 AQ_MAX_M, AQ_DECODE_MAX_M = 4096, 8
+AQ_KV8_BLOCK, AQ_KV8_MAX_SEQS, AQ_KV8_SCRATCH_BYTES = 32, 1024, 1 << 23
+AQ_ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+AQ_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 SYMBOLS = ("aq_pack", "aq_pack_opt", "aq_pack_sb", "aq_import_sb", "aq_export_sb", "aq_import", "aq_export", "aq_info", "aq_dequant", "aq_linear", "aq_linear_f32out", "aq_linear_noalloc",
            "aq_rbf_gram", "aq_hsic", "aq_sensitivity", "aq_allocate_bits",
            "aq_attn_scratch_bytes", "aq_rope", "aq_kv_append", "aq_attn_decode", "aq_stack_attn_scratch_bytes", "aq_stack_forward_attn",
+           "aq_kv8_plan", "aq_kv8_append", "aq_kv8_attn", "aq_rope_setup", "aq_rope_rows",
            "aq_stack_workspace_bytes", "aq_stack_forward", "aq_stack_buffer_offset", "aq_stack_input_offset", "aq_check", "aq_free",
            "aq_set_wait_limit_ns", "aq_debug_decode_hold", "aq_status_string", "aq_last_cuda_error", "aq_kernel_launches")
 
@@ -44,6 +48,31 @@ class Stack(C.Structure):
                 ("buf_width", C.POINTER(C.c_int64))]
 
 
+class _Kv8CacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int64),
+                ("page", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("pad_", C.c_int32)]
+
+
+class _Kv8BatchC(C.Structure):
+    _fields_ = [("lens", C.c_void_p), ("row_start", C.c_void_p), ("table", C.c_void_p), ("table_width", C.c_int64), ("n_seqs", C.c_int32),
+                ("pad_", C.c_int32)]
+
+
+class Rope(C.Structure):
+    """aq_rope_t: the frequencies of a rotary embedding (aq_rope_setup)."""
+    _fields_ = [("turns", C.c_double * 128), ("magnitude", C.c_float), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("pad_", C.c_int32)]
+
+
+_lib.aq_kv8_plan.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+_lib.aq_kv8_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_void_p]
+_lib.aq_kv8_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_float, C.c_int,
+                             C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.aq_rope_setup.argtypes = [C.c_int, C.c_int, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(Rope)]
+_lib.aq_rope_rows.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int,
+                              C.c_void_p, C.c_void_p]
+for _n in ("aq_kv8_plan", "aq_kv8_append", "aq_kv8_attn", "aq_rope_setup", "aq_rope_rows"):
+    getattr(_lib, _n).restype = C.c_int
 _lib.aq_pack.argtypes = [C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.POINTER(_H)]
 _lib.aq_pack_opt.argtypes = [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.POINTER(_H)]
 _lib.aq_pack_opt.restype = C.c_int
@@ -239,6 +268,151 @@ def aq_attn_decode(q, k_cache, v_cache, L: int, out, scratch, scale: float = 0.0
     _check(_lib.aq_attn_decode(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), M, H, Hkv, D, int(L), Lmax, float(scale),
                                dtype_code(q), dtype_code(out), _ptr(scratch), scratch.numel() * scratch.element_size(),
                                _stream(stream)), "aq_attn_decode")
+    return out
+
+
+# ---- a batch of requests over a paged cache held in 8 bits -----------------------------------------------------
+
+def _current_device() -> int:
+    """Index of torch's current device (first call: finds the cheapest way to ask and takes this function's place)."""
+    import torch
+    global _current_device
+    torch.cuda.current_device()
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _current_device()
+
+
+_INT = {}   # type code by torch's type, for the arrays that are not activations
+
+
+def _array(t, code, what):
+    """Address of an array of a step or a cache; refuses what the library would read wrongly."""
+    if not _INT:
+        import torch
+        _INT.update({torch.int8: "i8", torch.int32: "i32", torch.float32: "f32"})
+    if _INT.get(t.dtype) != code or not t.is_contiguous() or t.get_device() < 0:
+        raise ValueError(f"{what}: a contiguous CUDA tensor of type {code} is wanted, got {t.dtype} on {t.device}, strides {tuple(t.stride())}")
+    return t.data_ptr()
+
+
+def _rows(t, what):
+    """Address and row stride of a step's rows [n_rows][heads][head_dim]: rows may be apart, a row's heads lie together."""
+    T, H, D = t.shape
+    stride, per_head, one = t.stride()
+    if (one != 1 and D > 1) or (per_head != D and H > 1):
+        raise ValueError(f"{what}: the heads of a row have to lie together, got strides {(stride, per_head, one)} for shape {(T, H, D)}")
+    if t.get_device() != _current_device():
+        raise ValueError(f"{what}: on {t.device}, and the current device is cuda:{_current_device()}")
+    return t.data_ptr(), (stride if T > 1 else H * D)
+
+
+class Kv8Cache:
+    """A layer's keys and values in 8 bits: k, v CUDA int8 [n_pages][n_kv_heads][page][head_dim]; k_scale, v_scale CUDA float32
+    [n_pages][n_kv_heads][page / 32].  A value is code * scale.  Keeps the tensors; make it once."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "device", "c", "addr")
+
+    def __init__(self, k, v, k_scale, v_scale):
+        n, hkv, page, d = k.shape
+        want = (n, hkv, page // AQ_KV8_BLOCK)
+        if tuple(v.shape) != tuple(k.shape) or tuple(k_scale.shape) != want or tuple(v_scale.shape) != want:
+            raise ValueError(f"Kv8Cache: codes [n_pages][heads][page][dim] twice and scales [n_pages][heads][page / 32] twice are wanted, got "
+                             f"{tuple(k.shape)}, {tuple(v.shape)}, {tuple(k_scale.shape)}, {tuple(v_scale.shape)}")
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.get_device()
+        if {v.get_device(), k_scale.get_device(), v_scale.get_device()} != {self.device}:
+            raise ValueError("Kv8Cache: tensors of different devices")
+        self.c = _Kv8CacheC(_array(k, "i8", "k"), _array(v, "i8", "v"), _array(k_scale, "f32", "k_scale"), _array(v_scale, "f32", "v_scale"),
+                            n, page, hkv, d, 0)
+        self.addr = C.addressof(self.c)
+
+
+class Kv8Batch:
+    """A step: lens CUDA int32 [n_seqs] (new tokens included), table CUDA int32 [n_seqs][width], row_start CUDA int32 [n_seqs + 1] or None
+    (the same number of rows for each request).  Keeps the tensors; their contents may change from call to call."""
+
+    __slots__ = ("lens", "table", "row_start", "device", "c", "addr")
+
+    def __init__(self, lens, table, row_start=None):
+        n, width = table.shape
+        if tuple(lens.shape) != (n,) or (row_start is not None and tuple(row_start.shape) != (n + 1,)):
+            raise ValueError("Kv8Batch: lens [n], table [n][width] and row_start [n + 1] are wanted")
+        self.lens, self.table, self.row_start, self.device = lens, table, row_start, lens.get_device()
+        if table.get_device() != self.device or (row_start is not None and row_start.get_device() != self.device):
+            raise ValueError("Kv8Batch: tensors of different devices")
+        self.c = _Kv8BatchC(_array(lens, "i32", "lens"), None if row_start is None else _array(row_start, "i32", "row_start"),
+                            _array(table, "i32", "table"), width, n, 0)
+        self.addr = C.addressof(self.c)
+
+
+def _kv8_device(cache, batch, where):
+    dev = _current_device()
+    if cache.device != dev or batch.device != dev:
+        raise ValueError(f"{where}: cache on cuda:{cache.device}, step on cuda:{batch.device}, and the current device is cuda:{dev}")
+
+
+def aq_kv8_plan(lens, new, table, free, n_free, page: int, lens_out, n_free_out, row_start, pos, stream=None):
+    """All CUDA int32: lens, new, lens_out [n_seqs]; table [n_seqs][width]; free [capacity]; n_free, n_free_out [1]; row_start
+    [n_seqs + 1]; pos [n_rows]."""
+    n, width = table.shape
+    if not (lens.numel() == new.numel() == lens_out.numel() == n and row_start.numel() == n + 1 and n_free.numel() == n_free_out.numel() == 1):
+        raise ValueError("aq_kv8_plan: lens, new, lens_out [n], table [n][width], row_start [n + 1], n_free, n_free_out [1] are wanted")
+    dev = _current_device()
+    p = []
+    for t, what in ((lens, "lens"), (new, "new"), (table, "table"), (free, "free"), (n_free, "n_free"), (lens_out, "lens_out"),
+                    (n_free_out, "n_free_out"), (row_start, "row_start"), (pos, "pos")):
+        p.append(_array(t, "i32", what))
+        if t.get_device() != dev:
+            raise ValueError(f"aq_kv8_plan: {what} on {t.device}, and the current device is cuda:{dev}")
+    _check(_lib.aq_kv8_plan(p[0], p[1], n, int(page), p[2], width, p[3], free.numel(), p[4], p[5], p[6], p[7], p[8], pos.numel(),
+                            _stream(stream)), "aq_kv8_plan")
+
+
+def aq_kv8_append(cache: Kv8Cache, batch: Kv8Batch, k, v, stream=None):
+    """k, v: CUDA float16 / bfloat16 [n_rows][n_kv_heads][head_dim], rows of one stride."""
+    _kv8_device(cache, batch, "aq_kv8_append")
+    (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
+    if k.shape != v.shape or ks != vs or k.dtype != v.dtype or k.shape[1] != cache.c.n_kv_heads or k.shape[2] != cache.c.head_dim:
+        raise ValueError(f"aq_kv8_append: k and v are rows of {cache.c.n_kv_heads} heads of {cache.c.head_dim} alike, got {tuple(k.shape)} and {tuple(v.shape)}")
+    _check(_lib.aq_kv8_append(cache.addr, batch.addr, kp, vp, ks, k.shape[0], dtype_code(k), _stream(stream)), "aq_kv8_append")
+
+
+def aq_kv8_scratch(device=None):
+    """Scratch for aq_kv8_attn, zeroed (CUDA uint8)."""
+    import torch
+    return torch.zeros(AQ_KV8_SCRATCH_BYTES, dtype=torch.uint8, device=device or "cuda")
+
+
+def aq_kv8_attn(cache: Kv8Cache, batch: Kv8Batch, q, out, scratch, scale: float = 0.0, stream=None):
+    """q: CUDA float16 / bfloat16 [n_rows][n_heads][head_dim]; out: CUDA, the shape of q, any of the three types; scratch: CUDA uint8 of
+    AQ_KV8_SCRATCH_BYTES, zeroed before its first use (aq_kv8_scratch); calls that may overlap need scratch of their own."""
+    _kv8_device(cache, batch, "aq_kv8_attn")
+    (qp, qs), (op, os_) = _rows(q, "q"), _rows(out, "out")
+    if q.shape != out.shape or q.shape[2] != cache.c.head_dim or scratch.get_device() != cache.device:
+        raise ValueError(f"aq_kv8_attn: q and out are rows of heads of {cache.c.head_dim} alike, scratch on their device, got {tuple(q.shape)} and {tuple(out.shape)}")
+    _check(_lib.aq_kv8_attn(cache.addr, batch.addr, qp, qs, op, os_, q.shape[0], q.shape[1], float(scale), dtype_code(q), dtype_code(out),
+                            scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)), "aq_kv8_attn")
+    return out
+
+
+def aq_rope_setup(rot_dim: int, layout: str = "half", theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: float = 0.0,
+                  low: float = 0.0, high: float = 0.0, magnitude: float = 0.0) -> Rope:
+    """Host call.  layout: "half" or "pairs"; scaling: "none", "linear", "base" or "parts"."""
+    r = Rope()
+    _check(_lib.aq_rope_setup(int(rot_dim), AQ_ROPE_LAYOUTS[layout], float(theta), AQ_ROPE_SCALINGS[scaling], float(factor), float(trained),
+                              float(low), float(high), float(magnitude), C.byref(r)), "aq_rope_setup")
+    return r
+
+
+def aq_rope_rows(rope: Rope, x, pos, out=None, stream=None):
+    """x: CUDA [n_rows][n_heads][head_dim], any of the three types; pos: CUDA int32 [n_rows] (negative: the row is left as it is); out: like
+    x, of its type or, for float32, a half type; None: in place."""
+    out = x if out is None else out
+    (xp, xs), (op, os_) = _rows(x, "x"), _rows(out, "out")
+    T, H, D = x.shape
+    if out.shape != x.shape or pos.numel() != T or pos.get_device() != x.get_device():
+        raise ValueError(f"aq_rope_rows: out like x and a position per row are wanted, got {tuple(x.shape)}, {tuple(out.shape)}, {tuple(pos.shape)}")
+    _check(_lib.aq_rope_rows(C.byref(rope), xp, dtype_code(x), xs, op, dtype_code(out), os_, T, H, D, _array(pos, "i32", "pos"),
+                             _stream(stream)), "aq_rope_rows")
     return out
 
 

@@ -474,6 +474,113 @@ aq_status_t aq_attn_decode(const void* q_dev, const void* k_cache_dev, const voi
     return e == cudaSuccess ? AQ_OK : cuda_fail(e);
 }
 
+static inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static bool kv8_page_ok(int64_t page) { return page >= AQ_KV8_BLOCK && page <= 1024 && (page & (page - 1)) == 0; }
+static bool kv8_width_ok(int64_t width, int64_t page) { return width >= 1 && width <= (1 << 20) && width * page <= ((int64_t)1 << 30); }
+
+// A layer's cache and a step as aq_kv8_append and aq_kv8_attn take them.
+static aq_status_t kv8_args(const aq_kv8_cache_t* c, const aq_kv8_batch_t* b, int64_t n_rows) {
+    if (!c || !b || !c->k_dev || !c->v_dev || !c->k_scale_dev || !c->v_scale_dev || !aligned16(c->k_dev) || !aligned16(c->v_dev) ||
+        !aligned4(c->k_scale_dev) || !aligned4(c->v_scale_dev))
+        return AQ_ERR_INVALID_ARG;
+    if (!b->lens_dev || !b->table_dev || !aligned4(b->lens_dev) || !aligned4(b->table_dev) || !aligned4(b->row_start_dev)) return AQ_ERR_INVALID_ARG;
+    if (c->n_pages < 1 || c->n_pages > 0x7fffffff || c->n_kv_heads < 1 || !kv8_page_ok(c->page) || !kv8_width_ok(b->table_width, c->page) ||
+        b->n_seqs < 1 || n_rows < 1 || n_rows > AQ_MAX_M || (!b->row_start_dev && n_rows % b->n_seqs != 0))
+        return AQ_ERR_INVALID_ARG;
+    if (b->n_seqs > AQ_KV8_MAX_SEQS || c->n_kv_heads > 256 || (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)) return AQ_ERR_UNSUPPORTED;
+    return AQ_OK;
+}
+
+aq_status_t aq_kv8_plan(const int32_t* lens_dev, const int32_t* new_dev, int n_seqs, int page, int32_t* table_dev, int64_t table_width,
+                        int32_t* free_dev, int64_t free_cap, const int32_t* n_free_dev, int32_t* lens_out_dev, int32_t* n_free_out_dev,
+                        int32_t* row_start_dev, int32_t* pos_dev, int64_t n_rows, aq_stream_t stream) {
+    const void* all[] = {lens_dev, new_dev, table_dev, free_dev, n_free_dev, lens_out_dev, n_free_out_dev, row_start_dev, pos_dev};
+    for (const void* p : all)
+        if (!p || !aligned4(p)) return AQ_ERR_INVALID_ARG;
+    if (n_seqs < 1 || !kv8_page_ok(page) || !kv8_width_ok(table_width, page) || free_cap < 0 || free_cap > 0x7fffffff || n_rows < 1 || n_rows > (1 << 20))
+        return AQ_ERR_INVALID_ARG;
+    if (n_seqs > AQ_KV8_MAX_SEQS) return AQ_ERR_UNSUPPORTED;
+    aq_status_t st = check_arch(nullptr);
+    if (st != AQ_OK) return st;
+    const cudaError_t e = launch_kv8_plan(lens_dev, new_dev, n_seqs, page, table_dev, table_width, free_dev, free_cap, n_free_dev, lens_out_dev,
+                                          n_free_out_dev, row_start_dev, pos_dev, (int)n_rows, (cudaStream_t)stream);
+    return e == cudaSuccess ? AQ_OK : cuda_fail(e);
+}
+
+aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* k_dev, const void* v_dev, int64_t row_stride,
+                          int64_t n_rows, aq_dtype_t dtype, aq_stream_t stream) {
+    if (!k_dev || !v_dev || !aligned16(k_dev) || !aligned16(v_dev)) return AQ_ERR_INVALID_ARG;
+    if (dtype != AQ_F16 && dtype != AQ_BF16) return (dtype == AQ_F32) ? AQ_ERR_UNSUPPORTED : AQ_ERR_INVALID_ARG;
+    aq_status_t st = kv8_args(cache, batch, n_rows);
+    if (st != AQ_OK) return st;
+    if (row_stride % 8 != 0 || row_stride < (int64_t)cache->n_kv_heads * cache->head_dim || row_stride > ((int64_t)1 << 40)) return AQ_ERR_INVALID_ARG;
+    if ((st = check_arch(nullptr)) != AQ_OK) return st;
+    const cudaError_t e = launch_kv8_append(*cache, *batch, k_dev, v_dev, row_stride, (int)n_rows, dtype, (cudaStream_t)stream);
+    return e == cudaSuccess ? AQ_OK : cuda_fail(e);
+}
+
+aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* q_dev, int64_t q_stride, void* out_dev,
+                        int64_t out_stride, int64_t n_rows, int n_heads, float scale, aq_dtype_t dtype, aq_dtype_t out_dtype, void* scratch_dev,
+                        size_t scratch_bytes, aq_stream_t stream) {
+    if (!q_dev || !out_dev || !scratch_dev || !aligned16(q_dev) || !aligned16(out_dev) || (reinterpret_cast<uintptr_t>(scratch_dev) & 255u) ||
+        !std::isfinite(scale))
+        return AQ_ERR_INVALID_ARG;
+    if (dtype != AQ_F16 && dtype != AQ_BF16) return (dtype == AQ_F32) ? AQ_ERR_UNSUPPORTED : AQ_ERR_INVALID_ARG;
+    if (out_dtype != AQ_F16 && out_dtype != AQ_BF16 && out_dtype != AQ_F32) return AQ_ERR_INVALID_ARG;
+    aq_status_t st = kv8_args(cache, batch, n_rows);
+    if (st != AQ_OK) return st;
+    const int64_t row = (int64_t)n_heads * cache->head_dim, most = (int64_t)1 << 40;
+    if (n_heads < 1 || n_heads % cache->n_kv_heads != 0 || scratch_bytes < AQ_KV8_SCRATCH_BYTES || q_stride % 8 != 0 || out_stride % 8 != 0 ||
+        q_stride < row || out_stride < row || q_stride > most || out_stride > most)
+        return AQ_ERR_INVALID_ARG;
+    // the line of tiles (aq_kv8_runs.h) is counted in 32 bits
+    const int64_t groups = n_rows * (n_heads / cache->n_kv_heads) / 8 + batch->n_seqs, tiles = batch->table_width * (cache->page / AQ_KV8_BLOCK);
+    if (n_heads > (1 << 16) || (double)groups * tiles * cache->n_kv_heads >= 2147483648.0) return AQ_ERR_UNSUPPORTED;
+    if ((st = check_arch(nullptr)) != AQ_OK) return st;
+    if (!(scale > 0.f)) scale = 1.0f / std::sqrt((float)cache->head_dim);
+    const cudaError_t e = launch_kv8_attn(*cache, *batch, q_dev, q_stride, out_dev, out_stride, (int)n_rows, n_heads, scale, dtype, out_dtype,
+                                          scratch_dev, (cudaStream_t)stream);
+    return e == cudaSuccess ? AQ_OK : cuda_fail(e);
+}
+
+aq_status_t aq_rope_setup(int rot_dim, int layout, double theta, int scaling, double factor, double trained, double low, double high,
+                          double magnitude, aq_rope_t* out) {
+    if (!out || rot_dim < 2 || (rot_dim & 1) || rot_dim > 2 * AQ_ROPE_MAX_PAIRS || !(theta > 1.0) || !std::isfinite(theta) || !(factor >= 1.0) ||
+        !std::isfinite(factor) || !(magnitude >= 0.0) || !std::isfinite(magnitude))
+        return AQ_ERR_INVALID_ARG;
+    if ((layout != AQ_ROPE_HALF && layout != AQ_ROPE_PAIRS) || scaling < AQ_ROPE_NONE || scaling > AQ_ROPE_PARTS) return AQ_ERR_INVALID_ARG;
+    if (scaling == AQ_ROPE_PARTS) {
+        if (low == 0.0 && high == 0.0) { low = 1.0; high = 32.0; }
+        if (!(trained >= 1.0) || !std::isfinite(trained) || !(low >= 0.0) || !(high > low) || !std::isfinite(high)) return AQ_ERR_INVALID_ARG;
+    }
+    rope_setup(rot_dim, layout, theta, scaling, factor, trained, low, high, magnitude, out);
+    return AQ_OK;
+}
+
+aq_status_t aq_rope_rows(const aq_rope_t* rope, const void* x_dev, aq_dtype_t dtype, int64_t x_stride, void* out_dev, aq_dtype_t out_dtype,
+                         int64_t out_stride, int64_t n_rows, int n_heads, int head_dim, const int32_t* pos_dev, aq_stream_t stream) {
+    if (!rope || !x_dev || !out_dev || !pos_dev || !aligned4(pos_dev)) return AQ_ERR_INVALID_ARG;
+    const bool types = dtype == AQ_F16 || dtype == AQ_BF16 || dtype == AQ_F32, outs = out_dtype == AQ_F16 || out_dtype == AQ_BF16 || out_dtype == AQ_F32;
+    if (!types || !outs) return AQ_ERR_INVALID_ARG;
+    if (dtype != AQ_F32 && out_dtype != dtype) return AQ_ERR_UNSUPPORTED;
+    const uintptr_t in_size = dtype == AQ_F32 ? 4 : 2, out_size = out_dtype == AQ_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(x_dev) % in_size || reinterpret_cast<uintptr_t>(out_dev) % out_size) return AQ_ERR_INVALID_ARG;
+    if (rope->rot_dim < 2 || (rope->rot_dim & 1) || rope->rot_dim > 2 * AQ_ROPE_MAX_PAIRS || (rope->layout != AQ_ROPE_HALF && rope->layout != AQ_ROPE_PAIRS))
+        return AQ_ERR_INVALID_ARG;
+    if (n_rows < 1 || n_heads < 1 || head_dim < 2 || head_dim > (1 << 16) || n_heads > (1 << 16) || rope->rot_dim > head_dim ||
+        n_rows >= ((int64_t)1 << 31) / n_heads)
+        return AQ_ERR_INVALID_ARG;
+    const int64_t row = (int64_t)n_heads * head_dim, most = (int64_t)1 << 40;
+    if (x_stride < row || out_stride < row || x_stride > most || out_stride > most) return AQ_ERR_INVALID_ARG;
+    if (x_dev == out_dev && (dtype != out_dtype || x_stride != out_stride)) return AQ_ERR_INVALID_ARG;
+    aq_status_t st = check_arch(nullptr);
+    if (st != AQ_OK) return st;
+    const cudaError_t e = launch_rope_rows(*rope, x_dev, dtype, x_stride, out_dev, out_dtype, out_stride, (int)n_rows, n_heads, head_dim, pos_dev,
+                                           (cudaStream_t)stream);
+    return e == cudaSuccess ? AQ_OK : cuda_fail(e);
+}
+
 aq_status_t aq_allocate_bits(const double* S, const int64_t* numel, const int32_t* layer_of, int64_t n, const int32_t* types,
                              int n_types, double budget, int32_t* bits_out, double* objective_out) {
     if (!S || !numel || !layer_of || !types || !bits_out || n < 1 || n_types < 1 || !std::isfinite(budget)) return AQ_ERR_INVALID_ARG;
@@ -486,8 +593,8 @@ aq_status_t aq_allocate_bits(const double* S, const int64_t* numel, const int32_
 aq_status_t aq_check(aq_stream_t stream) {
     cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e);
-    const int g = read_gemm_status(true), d = read_decode_status(true), t = read_stage1_status(true);
-    return (g || d || t) ? AQ_ERR_TIMEOUT : AQ_OK;
+    const int g = read_gemm_status(true), d = read_decode_status(true), t = read_stage1_status(true), k = read_kv8_status(true);
+    return (g || d || t) ? AQ_ERR_TIMEOUT : k ? AQ_ERR_RANGE : AQ_OK;
 }
 
 aq_status_t aq_set_wait_limit_ns(uint64_t ns) {

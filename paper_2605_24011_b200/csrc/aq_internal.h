@@ -151,6 +151,19 @@ cudaError_t launch_attn_step(const float* q, const float* k, const float* v, voi
 cudaError_t launch_attn_angles(void* turn, int M, int64_t pos, float theta, cudaStream_t s);   // turn: M * 512 bytes
 cudaError_t launch_kv_append(void* kc, void* vc, const void* k, const void* v, int n_kv, int D, int64_t pos, int64_t Lmax, cudaStream_t s);
 
+// the paged 8-bit cache (aq_kv8.cu, aq_kv8_attn.cuh) and rotary rows (aq_rope_rows.cu)
+cudaError_t launch_kv8_plan(const int32_t* lens, const int32_t* added, int n_seqs, int page, int32_t* table, int64_t width, int32_t* free_list,
+                            int64_t free_cap, const int32_t* n_free, int32_t* lens_out, int32_t* n_free_out, int32_t* row_start, int32_t* pos,
+                            int n_rows, cudaStream_t s);
+cudaError_t launch_kv8_append(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, const void* k, const void* v, int64_t x_row, int T, aq_dtype_t dt,
+                              cudaStream_t s);
+cudaError_t launch_kv8_attn(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, const void* q, int64_t q_row, void* out, int64_t out_row, int T,
+                            int n_heads, float scale, aq_dtype_t dt, aq_dtype_t out_dt, void* scratch, cudaStream_t s);
+int read_kv8_status(bool clear);
+void rope_setup(int rot, int layout, double theta, int scaling, double factor, double trained, double low, double high, double magnitude, aq_rope_t* out);
+cudaError_t launch_rope_rows(const aq_rope_t& rope, const void* x, aq_dtype_t dt, int64_t x_row, void* out, aq_dtype_t out_dt, int64_t out_row,
+                             int rows, int heads, int D, const int32_t* pos, cudaStream_t s);
+
 // memory (aq_memory.cu): device blocks out of a bounded cache (null: no memory left; *held: the bytes the block really has, which is
 // what it is released with; idle: nothing on the device uses it any more); a copy into pageable host memory, complete when the
 // call returns
