@@ -182,7 +182,7 @@ aq_status_t aq_attn_decode(const void* q_dev, const void* k_cache_dev, const voi
  * aq_rope, aq_kv_append and aq_attn_decode.)
  *
  * The cache of a layer (aq_kv8_cache_t): codes, signed bytes [n_pages][n_kv_heads][page][head_dim] for keys and for values, and
- * one float32 scale per 32 positions of a page and head, [n_pages][n_kv_heads][page / 32]; a value is code * scale.  page: 32, 64,
+ * one float32 scale per 32 positions of a page and head, [n_pages][n_kv_heads][page / 32] (not negative); a value is code * scale.  page: 32, 64,
  * ... 1024; head_dim: 64, 128 or 256; 1 <= n_kv_heads <= 256.  A page can be used before anything was written to it: what lies
  * behind a request's length is never used.
  *
@@ -264,10 +264,11 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
  *   scratch_dev : DEVICE, 256-byte aligned, AQ_KV8_SCRATCH_BYTES, ZERO before its first use; a call leaves it as the next one wants it.
  *             Calls that may overlap in time (streams, captured graphs) need scratch of their own.
  * Built for decode (a few new tokens per request against long contexts); more rows per request are right but re-read the cache
- * for every 8 (head_dim 256) or 16 of a head's query rows.  Scores and sums are binary32; the weights enter the second product rounded to
- * binary16, those under 2^-40 of a row's largest as 0, and are summed as rounded: against the exact result for the cached values an output
- * is off by at most about 2^-10 sum_p softmax_p |V[p]|, 2^-18 of what the sum would be with every |V[p]| at its block's largest, and its own
- * rounding.  A query row with a NaN or an infinity gives NaN.
+ * for every 8 (head_dim 256) or 16 of a head's query rows.  A query row enters the products in 16 bits against its largest magnitude (off by
+ * 2^-16 of it at most), the products with the codes are exact, weights enter the second product in 16 bits against the largest of their 32
+ * positions (off by 2^-17 of that) and are summed as rounded, sums over positions are binary32: against the exact result for the
+ * cached values an output is off by at most about 2^-12 (sum_p softmax_p |V[p]| + what that sum would be with every |V[p]| at its block's
+ * largest), the scores' part and its own rounding.  A query row with a NaN or an infinity gives NaN.
  */
 aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* q_dev, int64_t q_stride, void* out_dev,
                         int64_t out_stride, int64_t n_rows, int n_heads, float scale, aq_dtype_t dtype, aq_dtype_t out_dtype, void* scratch_dev,

@@ -535,8 +535,8 @@ aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch
         q_stride < row || out_stride < row || q_stride > most || out_stride > most)
         return AQ_ERR_INVALID_ARG;
     // the line of tiles (aq_kv8_runs.h) is counted in 32 bits
-    const int64_t groups = n_rows * (n_heads / cache->n_kv_heads) / 8 + batch->n_seqs, tiles = batch->table_width * (cache->page / AQ_KV8_BLOCK);
-    if (n_heads > (1 << 16) || (double)groups * tiles * cache->n_kv_heads >= 2147483648.0) return AQ_ERR_UNSUPPORTED;
+    const int64_t groups = n_rows * (n_heads / cache->n_kv_heads) / 4 + batch->n_seqs, tiles = batch->table_width * (cache->page / AQ_KV8_BLOCK);
+    if (n_heads / cache->n_kv_heads > 256 || (double)groups * (tiles + 1) * cache->n_kv_heads >= 2147483648.0) return AQ_ERR_UNSUPPORTED;
     if ((st = check_arch(nullptr)) != AQ_OK) return st;
     if (!(scale > 0.f)) scale = 1.0f / std::sqrt((float)cache->head_dim);
     const cudaError_t e = launch_kv8_attn(*cache, *batch, q_dev, q_stride, out_dev, out_stride, (int)n_rows, n_heads, scale, dtype, out_dtype,

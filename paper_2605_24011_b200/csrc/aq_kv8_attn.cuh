@@ -4,19 +4,19 @@
 //
 // Bound: HBM.  Every key and value is read once, D bytes each; per position and head that is 2 D + 0.25 bytes for 4 D G M flops.
 //
-// Why this layout.  Positions are the rows of the tensor-core tile and query rows its columns (mma.sync.m16n8k16, binary16 in,
-// binary32 sums): with one to eight query rows per key/value head no part of a tile is padding but the columns, and a lane holds
-// two queries' scores, so a running maximum is two registers.  A tile of the work is 32 positions, the span of one scale, so the
-// scales touch the sums and not the operands.
-//   S^T = K q^T.  A code byte c + 128 in the low half of a binary16 IS the number (c + 128) 2^-24 (a subnormal): one byte permute
-//       per two codes makes the operand.  128 sum(q) is taken off the sum.  A lane's two bytes pairs of a 16-byte piece are dims
-//       4t .. 4t + 3 instead of 2t, 2t + 1, 2t + 8, 2t + 9: q is loaded in the same order.  q's row is divided by a power of two
-//       first so that its largest magnitude is in [1, 2): then bfloat16 rows fit binary16 too (what is under 2^-24 of the largest
-//       is lost, at most 2^-25 of it).
-//   P = exp2(S - max + 15), rounded to binary16 (weights down to 2^-39 of the largest keep a value), moved into operand order by
-//       movmatrix.  sum(P) is a product with ones, so the normaliser sums exactly what the values are weighted with.
-//   O^T += vs (V^T P^T - 128 sum P).  ldmatrix.trans on pairs of bytes gives dims 2g, 2g + 1 of two positions in one register:
-//       the even bytes are one operand row, the odd bytes another.
+// Why whole numbers.  The codes are signed bytes and so is what the tensor core multiplies (mma.sync.m16n8k32, 8-bit in, 32-bit sums,
+// as fast per instruction as its binary16 form with half the depth): keys go from the cache to the instruction as they are, values after
+// one byte permute per four codes; nothing is converted, and the sums are exact.  (With both made binary16 first, a tile of 128 dims took
+// 706 instructions per warp; the kernel waited for its own arithmetic: 32 x 4096 positions x 8 heads 62.6 us, DRAM 48 % busy.)
+//   A tile is 32 positions, the span of one scale, so scales touch the sums and not the operands.  Positions (or dims) are the 16 rows
+//   of the instruction and its 8 columns are four query rows in two planes, high and low byte:
+//   q^ = rint(q 32639 / max|q|) = 256 hi + lo, off by at most 2^-16 of the row's largest magnitude (a binary16 or bfloat16 q is
+//       itself known to 2^-12 or 2^-9 of each element).  hi and lo sums of a query lie in one lane: S = 256 hi + lo.
+//   P = rint(65535 exp2(S - the tile's largest S)): 16 bits against the tile's own largest weight, so a tile loses what lies under
+//       2^-17 of that and no tile is lost for being light.  Transposed by movmatrix and split into byte planes by a permute.  sum(P) is a
+//       product with ones: the normaliser sums what the values are weighted with.
+//   O = al O + vs fac (256 hi + lo) in binary32; ldmatrix.trans on pairs of bytes gives dims 2g, 2g + 1 of two positions per register.
+// A NaN (of a scale, of a query row) travels in the scales: F, fac.
 // Every warp has a contiguous run of the line of tiles (aq_kv8_runs.h) and streams it through its own cp.async ring without
 // waiting for another warp; runs differ by one tile at most whatever the requests' lengths are.  What a warp finishes alone it
 // writes; pieces of an item are merged over the warps of the CTA in shared memory, then over the CTAs in the scratch by the last
@@ -29,27 +29,28 @@ namespace aq {
 constexpr int KA_TILE = AQ_KV8_BLOCK;                 // positions per tile: the span of a scale
 constexpr int KA_MAX_CTAS = 192;
 
-template <int D, int NT>
+// QT: groups of four query rows.  A warp's ring holds TILES tiles, keys and values copied and waited for separately, each refilled when it has
+// been used.  The first of a run's items may leave a piece, which takes the place of a tile: the ring is one shorter from then on.
+template <int D, int QT>
 struct KaShape {
-    static constexpr int WARPS = D == 256 ? 4 : 8;
-    static constexpr int STAGES = D == 64 ? 5 : (NT == 2 ? 2 : 3);
-    static constexpr int ROWS = 8 * NT;               // query rows of an item
+    static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : D == 128 ? 8 : 6;
+    static constexpr int TILES = D == 256 ? 2 : 3;
+    static constexpr int ROWS = 4 * QT;               // query rows of an item
     static constexpr int HALF = KA_TILE * D;          // bytes of a tile's keys (or values)
-    static constexpr int STAGE = 2 * HALF + 16;       // + ks, vs, whether the tile may be read
+    static constexpr int BUF = HALF + 16;             // + their scale and, with the keys, whether the tile may be read
     static constexpr int PITCH = D + 4;               // floats: a row's O, then its maximum and sum
-    static constexpr int SLOT = ROWS * PITCH * 4;
-    static constexpr int RING = WARPS * STAGES * STAGE;
-    static constexpr int SMEM = RING + WARPS * SLOT;
-    static_assert(SLOT <= STAGES * STAGE, "a warp's last piece is put down in its own ring");
-    static_assert((AQ_KV8_MAX_SEQS + 1) * 4 <= WARPS * SLOT, "the line's marks lie where pieces will");
-    static_assert(WARPS * ROWS * D * 4 + KA_MAX_CTAS * ROWS * 8 <= RING, "the merge works in the ring");
-    static_assert(SMEM + 1024 <= 232448, "shared memory of an SM");
+    static constexpr int SLOT = ROWS * PITCH * 4;     // a piece
+    static constexpr int PLACE = 2 * BUF > SLOT ? 2 * BUF : SLOT;
+    static constexpr int RING = WARPS * TILES * PLACE;
+    static constexpr int SMEM = RING + ROWS * 32 * 12;   // + for merging: a weight, a maximum and a sum per row and part
+    static_assert((AQ_KV8_MAX_SEQS + 1) * 4 <= RING && 14 * SLOT <= RING, "the line's marks, and the parts of a group, lie in the ring");
+    static_assert(TILES >= 2 && 2 * WARPS <= 32, "a tile's place can be spared; a lane per piece");
+    static_assert(SMEM + 1300 <= 232448 && PLACE % 16 == 0, "shared memory of an SM");
 };
-// scratch: tickets [2][KA_MAX_CTAS][2], (maximum, sum) [KA_MAX_CTAS][2][rows], O [KA_MAX_CTAS][2][rows][D]
-constexpr size_t KA_TICKET_BYTES = 2 * KA_MAX_CTAS * 2 * 4;
-constexpr size_t KA_ML_BYTES = (size_t)KA_MAX_CTAS * 2 * 16 * 8;
-static_assert(KA_TICKET_BYTES + KA_ML_BYTES + (size_t)KA_MAX_CTAS * 2 * 8 * 256 * 4 <= AQ_KV8_SCRATCH_BYTES &&
-              KA_TICKET_BYTES + KA_ML_BYTES + (size_t)KA_MAX_CTAS * 2 * 16 * 128 * 4 <= AQ_KV8_SCRATCH_BYTES, "scratch");
+// scratch: tickets [2][KA_MAX_CTAS], parts [KA_MAX_CTAS][4][rows][pitch]
+constexpr size_t KA_TICKET_BYTES = 2 * KA_MAX_CTAS * 4;
+static_assert(KA_TICKET_BYTES % 16 == 0 && KA_TICKET_BYTES + (size_t)KA_MAX_CTAS * 4 * KaShape<128, 4>::SLOT <= AQ_KV8_SCRATCH_BYTES &&
+              KA_TICKET_BYTES + (size_t)KA_MAX_CTAS * 4 * KaShape<256, 2>::SLOT <= AQ_KV8_SCRATCH_BYTES, "scratch");
 
 struct KaArgs {
     const void* q;
@@ -64,11 +65,11 @@ struct KaArgs {
     int64_t width, n_pages, q_row, out_row;
     int B, T, n_each, Hkv, G;
     int shift;                  // log2(tiles per page)
+    uint32_t G_magic;           // for divisions by G
     int q_bf16, out_dtype;
     float scale_log2;           // scale log2(e)
     unsigned* tickets;
-    float* ml;
-    float* part;
+    uint8_t* part;
 };
 
 __device__ __forceinline__ void ka_cp16(uint32_t dst, const void* src) {
@@ -92,18 +93,19 @@ __device__ __forceinline__ uint32_t ka_transpose(uint32_t a) {
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-__device__ __forceinline__ void ka_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// signed rows x signed columns, signed rows x unsigned columns
+__device__ __forceinline__ void ka_mma_ss(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ka_mma_su(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float ka_exp2(float x) {   // 2 ulp; results below 2^-126 are 0
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-__device__ __forceinline__ uint32_t ka_pack(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
 }
 // Byte offset of 16-byte piece c of row r in a tile: rows of eight that ldmatrix reads together fall on different banks.
 template <int D>
@@ -125,19 +127,24 @@ __device__ __forceinline__ KaSeq ka_seq(const KaArgs& a, int b, int rows) {
     const int64_t most = a.width << (a.shift + 5);
     s.L = (int)min((int64_t)max(__ldg(a.lens + b), 0), most);
     s.nt = max(1, (s.L + KA_TILE - 1) / KA_TILE);   // (a request without positions has one tile that is not read: its rows become 0)
-    s.rb = (int)(((int64_t)s.n * a.G + rows - 1) / rows);
+    s.rb = (s.n * a.G + rows - 1) / rows;   // (n G <= 2^20)
     return s;
+}
+
+__device__ __forceinline__ uint32_t ka_places(const KaArgs& a, const KaSeq& s) {
+    return ((uint32_t)s.nt + KV8_ITEM_COST) * (uint32_t)s.rb * (uint32_t)a.Hkv;
 }
 
 // A piece of an item as it is put down for merging.
 struct KaPiece {
-    uint32_t start;   // the item's first tile on the line
+    uint32_t first;   // the place of the item's first tile on the line
     int nt;           // its tiles (0: no piece here)
     int row0, rows;   // first row of the request, its query rows (G n)
     int hk, q0;       // key/value head, the item's first query row
+    uint32_t at;      // where in shared memory
 };
 
-// Stores D/32 neighbouring values of a lane as the output's type.
+// N neighbouring values as the output's type
 template <int N>
 __device__ __forceinline__ void ka_store(const KaArgs& a, int64_t at, const float (&x)[N]) {
 #pragma unroll
@@ -148,78 +155,130 @@ __device__ __forceinline__ void ka_store(const KaArgs& a, int64_t at, const floa
     }
 }
 __device__ __forceinline__ int64_t ka_out_at(const KaArgs& a, int row0, int hk, int q, int D) {
-    const int tok = q / a.G;
+    const int tok = (int)kv8_div((uint32_t)q, a.G_magic);
     return (int64_t)(row0 + tok) * a.out_row + (int64_t)(hk * a.G + (q - tok * a.G)) * D;
 }
-// 2^24 over the normaliser (the sums of V are in units of 2^-24); a row that saw nothing is 0
-__device__ __forceinline__ float ka_norm(float l) { return l == 0.f ? 0.f : 16777216.f / l; }
+// one over the normaliser; a row that saw nothing is 0
+__device__ __forceinline__ float ka_norm(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
-template <int D, int NT>
-__global__ void __launch_bounds__(KaShape<D, NT>::WARPS * 32, 1) kv8_attn_kernel(const __grid_constant__ KaArgs a) {
-    using S = KaShape<D, NT>;
+// Arrives at an item's (or a group's) counter: whether this was the last of `want`, who puts it back to zero.  What the CTA wrote before
+// the barrier in front of this is visible to whoever arrives later, and what earlier ones wrote to this CTA after the next barrier.
+__device__ __forceinline__ bool ka_arrive(unsigned* ticket, unsigned one, unsigned want) {
+    unsigned was;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;" : "=r"(was) : "l"(ticket), "r"(one) : "memory");
+    const bool last = (one == 1u ? was & 0xffffu : was >> 16) == want - 1u;
+    if (last) atomicSub(ticket, one * want);
+    return last;
+}
+
+template <int D, int QT>
+__global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel(const __grid_constant__ KaArgs a) {
+    using S = KaShape<D, QT>;
     constexpr int W = S::WARPS, ROWS = S::ROWS, NV = D / 32;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ KaPiece pieces[2 * W];
-    __shared__ uint32_t warp_sum[W];
-    __shared__ int last_flag;
+    __shared__ uint32_t sums[W][2];
+    __shared__ int last_flag[2], group_head[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, t = lane & 3;
 
-    // ---- the line: marks[b] = first tile of request b -------------------------------------------------------
-    uint32_t* marks = reinterpret_cast<uint32_t*>(smem + S::RING);
+    // ---- the line: first place of each request ---------------------------------------------------------------
     pdl_wait();
-    {
-        const int per = (a.B + W * 32 - 1) / (W * 32), b0 = threadIdx.x * per;
-        uint32_t mine = 0;
-        for (int b = b0; b < min(b0 + per, a.B); ++b) {
-            const KaSeq s = ka_seq(a, b, ROWS);
-            if (s.n > 0 && s.L != __ldg(a.lens + b)) kv8_report(KV8_BAD_LENGTH);
-            mine += (uint32_t)s.nt * (uint32_t)s.rb * (uint32_t)a.Hkv;
+    pdl_launch_dependents();
+    if (lane < 2) pieces[2 * warp + lane].nt = 0;
+    uint32_t total, items;
+    KaSeq sq{};
+    uint32_t off = 0;             // the run's first place in its request
+    uint32_t n_cta, c0 = 0, c1 = 0, x0 = 0, x1 = 0;   // the CTA's share, the warp's run
+    Kv8Cut cut{};
+    auto my_run = [&] {
+        n_cta = kv8_ctas(total, items, W, gridDim.x);
+        if (blockIdx.x >= n_cta) return;
+        cut = kv8_cut(total, n_cta);
+        c0 = kv8_begin(cut, blockIdx.x);
+        c1 = kv8_begin(cut, blockIdx.x + 1);
+        x0 = kv8_warp_begin(c0, c1, warp, W);
+        x1 = kv8_warp_begin(c0, c1, warp + 1, W);
+    };
+    if (a.B <= 32) {   // a lane per request, in every warp: no warp waits for another
+        KaSeq s{};
+        if (lane < a.B) {
+            s = ka_seq(a, lane, ROWS);
+            if (s.n > 0 && s.L != __ldg(a.lens + lane)) kv8_report(KV8_BAD_LENGTH);
         }
+        const uint32_t mine = ka_places(a, s);
+        total = __reduce_add_sync(0xffffffffu, mine);
+        items = __reduce_add_sync(0xffffffffu, (unsigned)(s.rb * a.Hkv));
+        if (total == 0) return;
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d);
             if (lane >= d) upto += v;
         }
-        if (lane == 31) warp_sum[warp] = upto;
-        if (lane < 2) pieces[2 * warp + lane].nt = 0;
+        my_run();
+        if (blockIdx.x >= n_cta) return;
+        const unsigned here = __ballot_sync(0xffffffffu, upto - mine <= x0 && x0 < upto);
+        if (here) {
+            const int b = __ffs(here) - 1;
+            off = x0 - __shfl_sync(0xffffffffu, upto - mine, b);
+            sq.b = b;
+            sq.L = __shfl_sync(0xffffffffu, s.L, b); sq.row0 = __shfl_sync(0xffffffffu, s.row0, b); sq.n = __shfl_sync(0xffffffffu, s.n, b);
+            sq.nt = __shfl_sync(0xffffffffu, s.nt, b); sq.rb = __shfl_sync(0xffffffffu, s.rb, b);
+        }
+    } else {
+        uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
+        const int per = (a.B + W * 32 - 1) / (W * 32), b0 = threadIdx.x * per;
+        uint32_t mine = 0, my_items = 0;
+        for (int b = b0; b < min(b0 + per, a.B); ++b) {
+            const KaSeq s = ka_seq(a, b, ROWS);
+            if (s.n > 0 && s.L != __ldg(a.lens + b)) kv8_report(KV8_BAD_LENGTH);
+            mine += ka_places(a, s);
+            my_items += (uint32_t)s.rb * (uint32_t)a.Hkv;
+        }
+        uint32_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d), w = __shfl_up_sync(0xffffffffu, my_items, d);
+            if (lane >= d) { upto += v; my_items += w; }
+        }
+        if (lane == 31) { sums[warp][0] = upto; sums[warp][1] = my_items; }
         __syncthreads();
         uint32_t before = upto - mine;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
+        total = items = 0;
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) before += sums[w][0];
+            total += sums[w][0];
+            items += sums[w][1];
+        }
+        if (total == 0) return;
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             marks[b] = before;
-            const KaSeq s = ka_seq(a, b, ROWS);
-            before += (uint32_t)s.nt * (uint32_t)s.rb * (uint32_t)a.Hkv;
+            before += ka_places(a, ka_seq(a, b, ROWS));
         }
+        my_run();
+        if (blockIdx.x >= n_cta) return;
+        __syncthreads();
+        if (x0 < x1) {
+            const int b = kv8_find(marks, a.B, x0);
+            sq = ka_seq(a, b, ROWS);
+            off = x0 - marks[b];
+        }
+        __syncthreads();   // (the marks lie where tiles will)
     }
-    uint32_t total = 0;
-    for (int w = 0; w < W; ++w) total += warp_sum[w];
-    __syncthreads();
-    // CTAs with less than a tile per warp would only add pieces to merge
-    const uint32_t n_cta = min(gridDim.x, (total + W - 1) / W);
-    if (blockIdx.x >= n_cta) return;
-    const uint32_t n_run = n_cta * W, run = blockIdx.x * W + warp;
-    const uint32_t x0 = kv8_run_begin(total, run, n_run), x1 = kv8_run_begin(total, run + 1, n_run);
-    const uint32_t c0 = kv8_run_begin(total, blockIdx.x * W, n_run), c1 = kv8_run_begin(total, (blockIdx.x + 1) * W, n_run);
-
-    KaSeq sq{};
     int item = 0, j = 0;          // item of the request (head x block of rows), tile of the item
     if (x0 < x1) {
-        const int b = kv8_find(marks, a.B, x0);
-        sq = ka_seq(a, b, ROWS);
-        const uint32_t off = x0 - marks[b];
-        item = (int)(off / (uint32_t)sq.nt);
-        j = (int)(off - (uint32_t)item * (uint32_t)sq.nt);
+        const uint32_t len = (uint32_t)sq.nt + KV8_ITEM_COST;
+        item = (int)(off / len);
+        off -= (uint32_t)item * len;
+        if (off < KV8_ITEM_COST) x0 += KV8_ITEM_COST - off;   // (its first tile; past x1 if the run has none)
+        else j = (int)(off - KV8_ITEM_COST);
     }
-    __syncthreads();   // (pieces may be put down where the marks are)
 
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)warp * S::STAGES * S::STAGE;
-    float* slot_a = reinterpret_cast<float*>(smem + S::RING + warp * S::SLOT);
-    float* slot_b = reinterpret_cast<float*>(smem + warp * S::STAGES * S::STAGE);
+    const uint32_t my_ring = (uint32_t)(warp * S::TILES * S::PLACE), ring = (uint32_t)__cvta_generic_to_shared(smem) + my_ring;
 
     if (x0 < x1) {
-        // ---- copies: a walk of its own, STAGES - 1 tiles ahead ----------------------------------------------
+        // ---- copies: a walk of its own, TILES tiles ahead ----------------------------------------------------
         KaSeq ps = sq;
         int p_item = item, p_j = j, p_page0 = -1, p_pages = -1;   // lane i holds the number of page p_page0 + i
         uint32_t p_x = x0;
@@ -229,8 +288,53 @@ __global__ void __launch_bounds__(KaShape<D, NT>::WARPS * 32, 1) kv8_attn_kernel
             int b = s.b;
             do { s = ka_seq(a, ++b, ROWS); } while (s.n == 0 && b + 1 < a.B);   // (x < total: there is one)
         };
-        auto issue = [&](int st) {
-            const uint32_t dst = ring + (uint32_t)st * S::STAGE;
+        auto touch_queries = [&](const KaSeq& s, int it) {   // a line per lane, so that they are near when the item's turn comes
+            constexpr int LINES = D * 2 / 128;
+            const int hk = s.rb == 1 ? it : it / s.rb, r = (it - hk * s.rb) * ROWS + lane / LINES;
+            if (lane < ROWS * LINES && r < a.G * s.n) {
+                const int tok = (int)kv8_div((uint32_t)r, a.G_magic);
+                const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(s.row0 + tok) * a.q_row + (int64_t)(hk * a.G + (r - tok * a.G)) * D;
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(q + (lane % LINES) * 64));
+            }
+        };
+        // an item's query rows as they come: of row 4 u + g / 2, dims 32 c + 4 t .. and 16 further.  The first item's are asked for before its
+        // tiles where there are registers for that.
+        constexpr bool EARLY = QT * D <= 256;
+        uint2 raw[EARLY ? QT : 1][D / 32][2];
+        auto load_queries = [&](const KaSeq& s, int it, int u0) {
+            const int hk = s.rb == 1 ? it : it / s.rb, q0 = (it - hk * s.rb) * ROWS;
+#pragma unroll
+            for (int u = 0; u < (EARLY ? QT : 1); ++u) {
+                const int r = q0 + 4 * (u + u0) + (g >> 1);
+                if (r < a.G * s.n) {
+                    const int tok = (int)kv8_div((uint32_t)r, a.G_magic);
+                    const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(s.row0 + tok) * a.q_row +
+                                        (int64_t)(hk * a.G + (r - tok * a.G)) * D + 4 * t;
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        raw[u][c][0] = __ldg(reinterpret_cast<const uint2*>(q + 32 * c));
+                        raw[u][c][1] = __ldg(reinterpret_cast<const uint2*>(q + 32 * c + 16));
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) raw[u][c][0] = raw[u][c][1] = make_uint2(0u, 0u);
+                }
+            }
+        };
+        if constexpr (EARLY) load_queries(sq, item, 0);       // (under way while the first tiles' pages are looked up)
+        bool p_ok = false;
+        int64_t p_blk = 0;
+        auto copy = [&](uint32_t dst, const uint8_t* codes, const float* scales) {   // a tile's keys or values, and their scale
+            const uint8_t* src = codes + p_blk * S::HALF + lane * 16;
+            // (the rows' pattern repeats every eight: a few offsets of the lane, the rest is known when this is compiled)
+            constexpr int RPP = 512 / D, REP = RPP >= 8 ? 1 : 8 / RPP;
+#pragma unroll
+            for (int i = 0; i < S::HALF / 512; ++i)
+                ka_cp16(dst + ka_at<D>(lane / (D / 16) + i % REP * RPP, lane % (D / 16)) + i / REP * (REP * 512), src + i * 512);
+            if (lane == 0) ka_cp4(dst + S::HALF, scales + p_blk);
+        };
+        auto issue_keys = [&](int st) {
+            const uint32_t dst = ring + (uint32_t)(st * S::PLACE);
             const int pg = p_j >> a.shift;
             if (p_page0 < 0 || pg >= p_page0 + 32 || pg < p_page0) {
                 p_page0 = pg;
@@ -238,451 +342,428 @@ __global__ void __launch_bounds__(KaShape<D, NT>::WARPS * 32, 1) kv8_attn_kernel
                 p_pages = (int64_t)i < a.width && (i << (a.shift + 5)) < ps.L ? __ldg(a.table + (int64_t)ps.b * a.width + i) : -1;
             }
             const int page = __shfl_sync(0xffffffffu, p_pages, pg - p_page0);
-            const bool ok = page >= 0 && page < a.n_pages;
-            if (ok) {
-                const int hk = p_item / ps.rb;
-                const int64_t blk = (((int64_t)page * a.Hkv + hk) << a.shift) + (p_j & ((1 << a.shift) - 1));
-                const uint8_t* sk = a.kc + blk * S::HALF;
-                const uint8_t* sv = a.vc + blk * S::HALF;
-#pragma unroll
-                for (int i = 0; i < S::HALF / 512; ++i) {
-                    const int idx = i * 32 + lane, row = idx / (D / 16), c = idx % (D / 16);
-                    ka_cp16(dst + ka_at<D>(row, c), sk + idx * 16);
-                    ka_cp16(dst + S::HALF + ka_at<D>(row, c), sv + idx * 16);
-                }
-                if (lane < 2) ka_cp4(dst + 2 * S::HALF + 4 * lane, (lane ? a.vs : a.ks) + blk);
+            p_ok = page >= 0 && page < a.n_pages;
+            if (p_ok) {
+                const int hk = ps.rb == 1 ? p_item : p_item / ps.rb;
+                p_blk = (((int64_t)page * a.Hkv + hk) << a.shift) + (p_j & ((1 << a.shift) - 1));
+                copy(dst, a.kc, a.ks);
             } else if (ps.L > 0 && lane == 0) {
                 kv8_report(KV8_BAD_PAGE);
             }
-            if (lane == 2) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * S::HALF + 8), "r"(ok ? 1 : 0) : "memory");
-            if (++p_x < x1 && ++p_j == ps.nt) {
-                p_j = 0;
-                const int was = ps.b;
-                next_item(ps, p_item);
-                if (ps.b != was) p_page0 = -1;
+            if (lane == 1) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + S::HALF + 4), "r"(p_ok ? 1 : 0) : "memory");
+        };
+        auto issue_values = [&](int st) {   // of the tile whose keys were issued last; then on to the next
+            if (p_ok) copy(ring + (uint32_t)(st * S::PLACE + S::BUF), a.vc, a.vs);
+            ++p_x;
+            if (++p_j == ps.nt) {
+                p_x += KV8_ITEM_COST;
+                if (p_x < x1) {
+                    p_j = 0;
+                    const int was = ps.b;
+                    next_item(ps, p_item);
+                    if (ps.b != was) p_page0 = -1;
+                    touch_queries(ps, p_item);
+                }
             }
         };
-#pragma unroll
-        for (int s = 0; s < S::STAGES - 1; ++s) {
-            if (p_x < x1) issue(s);
+#pragma unroll 1
+        for (int s = 0; s < S::TILES; ++s) {
+            const bool more = p_x < x1;
+            if (more) issue_keys(s);
+            ka_commit();
+            if (more) issue_values(s);
             ka_commit();
         }
 
-        uint32_t qf[NT][D / 16][2];
-        float o[NT][D / 16][4];
-        float m[NT][2], l[NT][2], bq[NT][2], fq[NT][2];
-        int lim[NT][2], lim_min = 0;
+        uint32_t qf[QT][D / 32][2];
+        float o[QT][D / 16][2];       // of query row 4 u + t: dims 16 c + 2 g and the next
+        float m[QT], l[QT], fq[QT];
+        int lim[QT], lim_min = 0;
         KaPiece pc{};
         bool fresh = true;
-        int st = 0;
-        for (uint32_t x = x0; x < x1; ++x) {
+        int st = 0, gone = -1;        // the tile's place; the place that a piece has taken
+        for (uint32_t x = x0; x < x1;) {
             if (fresh) {   // ---- another item: its queries
                 fresh = false;
-                pc.start = x - (uint32_t)j;
+                pc.first = x - (uint32_t)j;
                 pc.nt = sq.nt;
                 pc.row0 = sq.row0;
                 pc.rows = a.G * sq.n;
-                pc.hk = item / sq.rb;
+                pc.hk = sq.rb == 1 ? item : item / sq.rb;
                 pc.q0 = (item - pc.hk * sq.rb) * ROWS;
+                // operand column g of a group of four rows: row g / 2, plane g % 2
+                if constexpr (EARLY) { if (x != x0) load_queries(sq, item, 0); }
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int r = pc.q0 + 8 * nt + g;   // this lane's operand column
-                    uint2 raw[D / 16];
-                    if (r < pc.rows) {
-                        const int tok = r / a.G;
-                        const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(pc.row0 + tok) * a.q_row +
-                                            (int64_t)(pc.hk * a.G + (r - tok * a.G)) * D + 4 * t;
+                for (int u = 0; u < QT; ++u) {
+                    if constexpr (!EARLY) load_queries(sq, item, u);
+                    constexpr int U = EARLY ? 1 : 0;   // (whether raw holds all groups)
+                    // magnitudes as whole numbers: of two values of one type the larger has the larger pattern, a NaN the largest
+                    uint32_t most = 0;
 #pragma unroll
-                        for (int c = 0; c < D / 16; ++c) raw[c] = __ldg(reinterpret_cast<const uint2*>(q + 16 * c));
+                    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) most = __vmaxu2(most, __vmaxu2(raw[u * U][c][h].x & 0x7fff7fffu, raw[u * U][c][h].y & 0x7fff7fffu));
+                    most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                    most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                    most = max(most & 0xffffu, most >> 16);
+                    const bool poison = most >= (a.q_bf16 ? 0x7f80u : 0x7c00u);
+                    const float big = a.q_bf16 ? __uint_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
+                    const float up = poison ? 0.f : fminf(__fdividef(32638.9f, big), 3e38f);   // (rows of zeros: 0 times the largest number)
+                    // q up + 1.5 * 2^23 has rint(q up) in its low bits; 128 more, and the second byte is the high plane's
+                    const float magic = 12582912.f + ((g & 1) ? 0.f : 128.f);
+                    const uint32_t pick = (g & 1) ? 0x0040 : 0x0051;
+                    auto planes = [&](float y0, float y1, float y2, float y3) -> uint32_t {
+                        const uint32_t n0 = __float_as_uint(fmaf(y0, up, magic)), n1 = __float_as_uint(fmaf(y1, up, magic));
+                        const uint32_t n2 = __float_as_uint(fmaf(y2, up, magic)), n3 = __float_as_uint(fmaf(y3, up, magic));
+                        return __byte_perm(__byte_perm(n0, n1, pick), __byte_perm(n2, n3, pick), 0x5410);
+                    };
+                    if (a.q_bf16) {
+                        auto w = [](uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); };
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float2 e = w(raw[u * U][c][h].x), f = w(raw[u * U][c][h].y);
+                                qf[u][c][h] = planes(e.x, e.y, f.x, f.y);
+                            }
                     } else {
 #pragma unroll
-                        for (int c = 0; c < D / 16; ++c) raw[c] = make_uint2(0u, 0u);
-                    }
-                    auto wide = [&](uint32_t v) -> float2 {
-                        if (a.q_bf16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-                        return __half22float2(*reinterpret_cast<const __half2*>(&v));
-                    };
-                    float big = 0.f;
+                        for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        const float2 u = wide(raw[c].x), v = wide(raw[c].y);
-                        big = fmaxf(big, fmaxf(fmaxf(fabsf(u.x), fabsf(u.y)), fmaxf(fabsf(v.x), fabsf(v.y))));
+                            for (int h = 0; h < 2; ++h) {
+                                const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&raw[u * U][c][h].x));
+                                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&raw[u * U][c][h].y));
+                                qf[u][c][h] = planes(e.x, e.y, f.x, f.y);
+                            }
                     }
-                    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-                    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-                    // the power of two under the largest magnitude, as a factor that takes it off (1 for rows of zeros; an infinity stays one)
-                    const int e = big > 0.f ? min(max((int)(__float_as_uint(big) >> 23), 1), 253) : 127;
-                    const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
-                    float sum = 0.f;
+                    // of the query row whose scores this lane holds (row t of the group: lanes of columns 2t and 2t + 1 have it)
+                    const float step = poison ? __uint_as_float(0x7fc00000u) : __fdividef(big, 32638.9f);
+                    fq[u] = __shfl_sync(0xffffffffu, step, 8 * t) * a.scale_log2;
+                    lim[u] = sq.L - sq.n + (int)kv8_div((uint32_t)min(pc.q0 + 4 * u + t, pc.rows - 1), a.G_magic) + 1;   // positions before this one are seen
+                    m[u] = -INFINITY;
+                    l[u] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        const float2 u = wide(raw[c].x), v = wide(raw[c].y);
-                        qf[nt][c][0] = ka_pack(u.x * down, u.y * down);
-                        qf[nt][c][1] = ka_pack(v.x * down, v.y * down);
-                        const float2 a2 = __half22float2(*reinterpret_cast<const __half2*>(&qf[nt][c][0]));
-                        const float2 b2 = __half22float2(*reinterpret_cast<const __half2*>(&qf[nt][c][1]));
-                        sum += (a2.x + a2.y) + (b2.x + b2.y);
-                    }
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                    sum *= 128.f / 16777216.f;   // what the codes' offset of 128 adds to this row's products
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {   // and of the two query rows whose scores this lane holds
-                        bq[nt][i] = __shfl_sync(0xffffffffu, sum, 4 * (2 * t + i));
-                        fq[nt][i] = __shfl_sync(0xffffffffu, up, 4 * (2 * t + i)) * (a.scale_log2 * 16777216.f);
-                        const int rr = min(pc.q0 + 8 * nt + 2 * t + i, pc.rows - 1);
-                        lim[nt][i] = sq.L - sq.n + rr / a.G + 1;   // positions before this one are seen
-                        m[nt][i] = -INFINITY;
-                        l[nt][i] = 0.f;
-                    }
-#pragma unroll
-                    for (int c = 0; c < D / 16; ++c) o[nt][c][0] = o[nt][c][1] = o[nt][c][2] = o[nt][c][3] = 0.f;
+                    for (int c = 0; c < D / 16; ++c) o[u][c][0] = o[u][c][1] = 0.f;
                 }
-                lim_min = sq.L - sq.n + pc.q0 / a.G + 1;
+                lim_min = sq.L - sq.n + (int)kv8_div((uint32_t)pc.q0, a.G_magic) + 1;
             }
 
-            ka_wait<S::STAGES - 2>();
-            __syncwarp();   // every lane's copies of this tile have landed, and every lane is through with the tile before
-            if (p_x < x1) issue(st == 0 ? S::STAGES - 1 : st - 1);
-            ka_commit();
-            const uint32_t kt = ring + (uint32_t)st * S::STAGE, vt = kt + S::HALF;
-            st = st + 1 == S::STAGES ? 0 : st + 1;
-            float ks, vs;
+            const bool item_ends = j + 1 == sq.nt;
+            const uint32_t next = x + 1 + (item_ends ? KV8_ITEM_COST : 0u);
+            const bool run_ends = next >= x1, whole = item_ends && pc.first >= x0, take = item_ends && !run_ends && !whole;
+            if (gone < 0) ka_wait<2 * S::TILES - 1>(); else ka_wait<2 * S::TILES - 3>();
+            __syncwarp();   // every lane's copies of the keys have landed
+            const uint32_t kt = ring + (uint32_t)(st * S::PLACE), vt = kt + S::BUF;
+            float ks;
             int ok;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(kt + 2 * S::HALF) : "memory");
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(kt + 2 * S::HALF + 4) : "memory");
-            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(ok) : "r"(kt + 2 * S::HALF + 8) : "memory");
-
-            if (ok) {   // (the same for all lanes; a tile that could not be read counts as masked)
-                // ---- S^T = K q^T: 32 positions x 8 NT queries
-                float sc[NT][2][4];
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(kt + S::HALF) : "memory");
+            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(ok) : "r"(kt + S::HALF + 4) : "memory");
+            // (ok is the same for all lanes; a tile that could not be read counts as masked)
+            int sc[QT][2][4];
+            if (ok) {
+                // ---- S = K q: 32 positions x 4 QT query rows x 2 planes
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int u = 0; u < QT; ++u)
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) sc[nt][mt][0] = sc[nt][mt][1] = sc[nt][mt][2] = sc[nt][mt][3] = 0.f;
+                    for (int mt = 0; mt < 2; ++mt) sc[u][mt][0] = sc[u][mt][1] = sc[u][mt][2] = sc[u][mt][3] = 0;
 #pragma unroll
-                for (int cp = 0; cp < D / 32; ++cp) {
+                for (int c = 0; c < D / 32; ++c) {
 #pragma unroll
                     for (int mt = 0; mt < 2; ++mt) {
                         uint32_t r[4];
-                        ka_ldm(kt + ka_at<D>(16 * mt + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * cp + (lane >> 4)), r);
+                        ka_ldm(kt + ka_at<D>(16 * mt + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * c + (lane >> 4)), r);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) r[i] ^= 0x80808080u;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t a0 = __byte_perm(r[2 * h], 0u, 0x4140), a2 = __byte_perm(r[2 * h], 0u, 0x4342);
-                            const uint32_t a1 = __byte_perm(r[2 * h + 1], 0u, 0x4140), a3 = __byte_perm(r[2 * h + 1], 0u, 0x4342);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) ka_mma(sc[nt][mt], a0, a1, a2, a3, qf[nt][2 * cp + h][0], qf[nt][2 * cp + h][1]);
-                        }
+                        for (int u = 0; u < QT; ++u) ka_mma_ss(sc[u][mt], r, qf[u][c][0], qf[u][c][1]);
                     }
                 }
+            }
+            __syncwarp();   // every lane is through with the keys
+            const bool more = p_x < x1 && !take;
+            if (more) issue_keys(st);
+            if (take) ka_wait<2 * S::TILES - 2>();
+            else {
+                ka_commit();
+                if (gone < 0) ka_wait<2 * S::TILES - 1>(); else ka_wait<2 * S::TILES - 3>();
+            }
+            __syncwarp();   // every lane's copies of the values have landed
+            if (ok) {
+                float vs;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(vt + S::HALF) : "memory");
                 // ---- weights
                 const int pos = j * KA_TILE;
                 const bool all_seen = pos + KA_TILE <= lim_min;
-                uint32_t pb[NT][2][2];
-                float al[NT][2], vq[NT][2], off[NT][2];
+                uint32_t pb[QT][2];
+                float al[QT], vf[QT];
                 bool moved = false;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
+                for (int u = 0; u < QT; ++u) {
+                    int s[4];   // positions g, g + 8, g + 16, g + 24 of row t
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[i] = sc[u][i >> 1][2 * (i & 1)] * 256 + sc[u][i >> 1][2 * (i & 1) + 1];
+                    constexpr int NONE = -0x7fffffff - 1;   // (no score is so low: |S| <= 256 * 127 * (256 * 127 + 127))
                     if (!all_seen) {
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (pos + 16 * mt + (i >> 1) * 8 + g >= lim[nt][i & 1]) sc[nt][mt][i] = -INFINITY;
+                        for (int i = 0; i < 4; ++i) s[i] = pos + 8 * i + g < lim[u] ? s[i] : NONE;
                     }
-                    float base[2];
+                    int top = max(max(s[0], s[1]), max(s[2], s[3]));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                    const float F = ks * fq[u];
+                    uint32_t p[4];   // the low half: rint(65535 weight)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float mx = fmaxf(fmaxf(sc[nt][0][i], sc[nt][0][i + 2]), fmaxf(sc[nt][1][i], sc[nt][1][i + 2]));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        const float F = ks * fq[nt][i];
-                        const float s = mx == -INFINITY ? -INFINITY : (mx - bq[nt][i]) * F;
-                        const float now = fmaxf(m[nt][i], s);   // (a NaN among the scores leaves the maximum and reaches the sums)
-                        base[i] = now == -INFINITY ? 0.f : now;
-                        al[nt][i] = ka_exp2(m[nt][i] - base[i]);
-                        moved |= now != m[nt][i];
-                        m[nt][i] = now;
-                        const float add = 15.f - base[i];
-#pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                            for (int k = i; k < 4; k += 2) {
-                                const float raw = sc[nt][mt][k];
-                                const float p = ka_exp2(fmaf(raw - bq[nt][i], F, add));
-                                sc[nt][mt][k] = raw == -INFINITY ? 0.f : p;
-                            }
+                    for (int i = 0; i < 4; ++i) {
+                        const float w = ka_exp2((float)(int)((uint32_t)s[i] - (uint32_t)top) * F);
+                        p[i] = __float_as_uint(fmaf(w, 65535.f, 8388608.f));
+                        if (!all_seen && s[i] == NONE) p[i] = 0u;
                     }
-                    float lt[4] = {0.f, 0.f, 0.f, 0.f};
+                    int lt[4] = {0, 0, 0, 0};
+                    const uint32_t ones[4] = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) {
-                        pb[nt][mt][0] = ka_transpose(ka_pack(sc[nt][mt][0], sc[nt][mt][1]));
-                        pb[nt][mt][1] = ka_transpose(ka_pack(sc[nt][mt][2], sc[nt][mt][3]));
-                        ka_mma(lt, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, pb[nt][mt][0], pb[nt][mt][1]);
+                    for (int h = 0; h < 2; ++h) {
+                        // columns 2t, 2t + 1: row t's positions g and g + 8; transposed, lane (g, t) has two of the four positions 2t, 2t + 1, 2t + 8,
+                        // 2t + 9 of row g / 2 and its neighbour the other two: even g takes the four high bytes, odd g the low ones
+                        const uint32_t mine = ka_transpose(__byte_perm(p[2 * h], p[2 * h + 1], 0x5410));
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 4);
+                        pb[u][h] = __byte_perm(mine, other, (g & 1) ? 0x2064 : 0x7531);
                     }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        l[nt][i] = fmaf(l[nt][i], al[nt][i], lt[i]);
-                        off[nt][i] = lt[i] * (-128.f / 16777216.f);
-                        vq[nt][i] = lt[i] == 0.f ? 0.f : vs;   // (what a row gives no weight cannot reach it, a NaN among it)
-                    }
+                    ka_mma_su(lt, ones, pb[u][0], pb[u][1]);
+                    const bool any = top != NONE;
+                    const float s_top = any ? (float)top * F : -INFINITY;
+                    const float now = fmaxf(m[u], s_top);   // (a NaN leaves the maximum; fac carries it into the sums)
+                    al[u] = now == -INFINITY ? 1.f : ka_exp2(m[u] - now);
+                    const float fac = any ? ka_exp2(s_top - (now == -INFINITY ? 0.f : now)) : 0.f;
+                    moved |= now != m[u];
+                    m[u] = now;
+                    l[u] = fmaf(l[u], al[u], (float)(lt[0] * 256 + lt[1]) * fac);
+                    vf[u] = any ? vs * fac : 0.f;   // (what a row does not see cannot reach it, a NaN among it)
                 }
                 moved = __any_sync(0xffffffffu, moved);
-                // ---- O^T = al O^T + vs (V^T P^T - 128 sum P)
+                if (moved) {
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c) { o[u][c][0] *= al[u]; o[u][c][1] *= al[u]; }
+                }
+                // ---- O += vs fac V P
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     uint32_t r[4];
                     ka_ldm_t(vt + ka_at<D>(lane, c), r);
+                    // rows 0..7 are even dims, 8..15 odd ones; depth: positions 2t, 2t + 1, 2t + 8, 2t + 9, then those + 16
+                    const uint32_t v[4] = {__byte_perm(r[0], r[1], 0x6420), __byte_perm(r[0], r[1], 0x7531), __byte_perm(r[2], r[3], 0x6420),
+                                           __byte_perm(r[2], r[3], 0x7531)};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) r[i] ^= 0x80808080u;
-                    uint32_t ev[4], od[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        ev[i] = __byte_perm(r[i], 0u, 0x4240);
-                        od[i] = __byte_perm(r[i], 0u, 0x4341);
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        float ot[4] = {off[nt][0], off[nt][1], off[nt][0], off[nt][1]};
-                        ka_mma(ot, ev[0], od[0], ev[1], od[1], pb[nt][0][0], pb[nt][0][1]);
-                        ka_mma(ot, ev[2], od[2], ev[3], od[3], pb[nt][1][0], pb[nt][1][1]);
-                        if (moved) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[nt][c][i] *= al[nt][i & 1];
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[nt][c][i] = fmaf(vq[nt][i & 1], ot[i], o[nt][c][i]);
+                    for (int u = 0; u < QT; ++u) {
+                        int ot[4] = {0, 0, 0, 0};
+                        ka_mma_su(ot, v, pb[u][0], pb[u][1]);
+                        o[u][c][0] = fmaf(vf[u], (float)(ot[0] * 256 + ot[1]), o[u][c][0]);
+                        o[u][c][1] = fmaf(vf[u], (float)(ot[2] * 256 + ot[3]), o[u][c][1]);
                     }
                 }
             }
+            __syncwarp();   // every lane is through with the values
+            if (more) issue_values(st);
+            if (!take) ka_commit();
 
             // ---- the item's end, or the run's
-            const bool item_ends = j + 1 == sq.nt, run_ends = x + 1 == x1;
             if (item_ends || run_ends) {
-                const bool whole = item_ends && pc.start >= x0;
                 if (whole) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int u = 0; u < QT; ++u) {
+                        const int r = pc.q0 + 4 * u + t;
+                        if (r < pc.rows) {
+                            const float inv = ka_norm(l[u]);
+                            const int64_t at = ka_out_at(a, pc.row0, pc.hk, r, D) + 2 * g;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int r = pc.q0 + 8 * nt + 2 * t + i;
-                            if (r < pc.rows) {
-                                const float inv = ka_norm(l[nt][i]);
-                                const int64_t at = ka_out_at(a, pc.row0, pc.hk, r, D) + 2 * g;
-#pragma unroll
-                                for (int c = 0; c < D / 16; ++c) {
-                                    const float two[2] = {o[nt][c][i] * inv, o[nt][c][i + 2] * inv};
-                                    ka_store(a, at + 16 * c, two);
-                                }
+                            for (int c = 0; c < D / 16; ++c) {
+                                const float two[2] = {o[u][c][0] * inv, o[u][c][1] * inv};
+                                ka_store(a, at + 16 * c, two);
                             }
                         }
+                    }
                 } else {
-                    // a run's first piece goes to a place of its own, its last into the ring, which is done with by then
-                    if (run_ends) { ka_wait<0>(); __syncwarp(); }
-                    float* to = run_ends ? slot_b : slot_a;
+                    // the run's first piece, where this tile was, or its last: all copies have been used by then
+                    pc.at = my_ring + (uint32_t)(st * S::PLACE);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int u = 0; u < QT; ++u) {
+                        float* row = reinterpret_cast<float*>(smem + pc.at) + (4 * u + t) * S::PITCH;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float* row = to + (8 * nt + 2 * t + i) * S::PITCH;
-#pragma unroll
-                            for (int c = 0; c < D / 16; ++c) *reinterpret_cast<float2*>(row + 16 * c + 2 * g) = make_float2(o[nt][c][i], o[nt][c][i + 2]);
-                            if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(m[nt][i], l[nt][i]);
-                        }
+                        for (int c = 0; c < D / 16; ++c) *reinterpret_cast<float2*>(row + 16 * c + 2 * g) = make_float2(o[u][c][0], o[u][c][1]);
+                        if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(m[u], l[u]);
+                    }
                     if (lane == 0) pieces[2 * warp + (run_ends ? 1 : 0)] = pc;
+                    if (take) gone = st;
                 }
             }
+            st = st + 1 == S::TILES ? 0 : st + 1;
+            if (st == gone) st = st + 1 == S::TILES ? 0 : st + 1;
             if (item_ends) {
                 j = 0;
                 if (!run_ends) { next_item(sq, item); fresh = true; }
             } else {
                 ++j;
             }
+            x = next;
         }
         ka_wait<0>();
     }
     __syncthreads();
 
-    // ---- pieces of one item lie next to each other in the order of the warps: merge them -----------------------
-    // A piece of an item that other CTAs have parts of goes to the scratch: place 0 if the item holds the CTA's first tile, else 1.
-    KaPiece open[2];
-    open[0].nt = open[1].nt = 0;
-    {
-        int e = 0, seq = 0;
-        while (e < 2 * W) {
-            if (pieces[e].nt == 0) { ++e; continue; }
-            const KaPiece pc = pieces[e];
-            int e1 = e + 1;
-            while (e1 < 2 * W && (pieces[e1].nt == 0 || pieces[e1].start == pc.start)) ++e1;
-            const bool whole = pc.start >= c0 && pc.start + (uint32_t)pc.nt <= c1;
-            const int place = pc.start <= c0 ? 0 : 1;
-            if (!whole) open[place] = pc;
-            for (int r = 0; r < min(ROWS, pc.rows - pc.q0); ++r, ++seq) {
-                if (seq % W != warp) continue;
-                float top = -INFINITY;
-                for (int i = e; i < e1; ++i)
-                    if (pieces[i].nt) {
-                        const float* row = ((i & 1) ? reinterpret_cast<float*>(smem + (i >> 1) * S::STAGES * S::STAGE)
-                                                    : reinterpret_cast<float*>(smem + S::RING + (i >> 1) * S::SLOT)) + r * S::PITCH;
-                        top = fmaxf(top, row[D]);
-                    }
-                const float base = top == -INFINITY ? 0.f : top;
-                float acc[NV], ls = 0.f;
+    // ---- merging ---------------------------------------------------------------------------------------------
+    // Up to 32 parts in shared memory, part k at byte my_at of lane k, neighbours of one item in groups that begin at the lanes of `heads`:
+    // first every part's weight (a warp per row, a lane per part), then the sums (a thread per four dims).
+    float2 (*stat)[32] = reinterpret_cast<float2 (*)[32]>(smem + S::RING);
+    float (*weight)[32] = reinterpret_cast<float (*)[32]>(smem + S::RING + ROWS * 32 * 8);
+    auto weigh = [&](unsigned there, unsigned heads, uint32_t my_at, int rows) {
+        const unsigned upto = heads & ((2u << lane) - 1u), later = heads & ~((2u << lane) - 1u);
+        const int lo = upto ? 31 - __clz(upto) : 0, hi = later ? __ffs(later) - 2 : 31;
+        for (int r = warp; r < rows; r += W) {
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (there >> lane & 1u) ml = *reinterpret_cast<const float2*>(smem + my_at + (r * S::PITCH + D) * 4);
+            float top = ml.x;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) acc[v] = 0.f;
-                for (int i = e; i < e1; ++i)
-                    if (pieces[i].nt) {
-                        const float* row = ((i & 1) ? reinterpret_cast<float*>(smem + (i >> 1) * S::STAGES * S::STAGE)
-                                                    : reinterpret_cast<float*>(smem + S::RING + (i >> 1) * S::SLOT)) + r * S::PITCH;
-                        const float w = ka_exp2(row[D] - base);
-                        ls = fmaf(w, row[D + 1], ls);
-#pragma unroll
-                        for (int v = 0; v < NV; v += 2) {
-                            const float2 y = *reinterpret_cast<const float2*>(row + NV * lane + v);
-                            acc[v] = fmaf(w, y.x, acc[v]);
-                            acc[v + 1] = fmaf(w, y.y, acc[v + 1]);
-                        }
-                    }
-                if (whole) {
-                    const float inv = ka_norm(ls);
-#pragma unroll
-                    for (int v = 0; v < NV; ++v) acc[v] *= inv;
-                    ka_store(a, ka_out_at(a, pc.row0, pc.hk, pc.q0 + r, D) + NV * lane, acc);
-                } else {
-                    const size_t at = ((size_t)blockIdx.x * 2 + place) * ROWS + r;
-#pragma unroll
-                    for (int v = 0; v < NV; v += 2) __stcg(reinterpret_cast<float2*>(a.part + at * D + NV * lane + v), make_float2(acc[v], acc[v + 1]));
-                    if (lane == 0) __stcg(reinterpret_cast<float2*>(a.ml) + at, make_float2(top, ls));
-                }
+            for (int d = 1; d < 32; d <<= 1) {
+                const float v = __shfl_up_sync(0xffffffffu, top, d);
+                if (lane - d >= lo) top = fmaxf(top, v);
             }
-            e = e1;
+            top = __shfl_sync(0xffffffffu, top, hi);
+            const float w = ka_exp2(ml.x - (top == -INFINITY ? 0.f : top));
+            float l = ml.y * w;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const float v = __shfl_up_sync(0xffffffffu, l, d);
+                if (lane - d >= lo) l += v;
+            }
+            l = __shfl_sync(0xffffffffu, l, hi);
+            weight[r][lane] = w;
+            if (lane == lo) stat[r][lane] = make_float2(top, l);
+        }
+    };
+    auto sum_parts = [&](unsigned there, int k0, int k1, int r, int d, auto at) -> float4 {   // parts k0 .. k1 - 1, those of `there`
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = k0; k < k1; ++k) {
+            if (!(there >> k & 1u)) continue;
+            const float4 y = *reinterpret_cast<const float4*>(smem + at(k) + (r * S::PITCH + d) * 4);
+            const float w = weight[r][k];
+            o.x = fmaf(w, y.x, o.x); o.y = fmaf(w, y.y, o.y); o.z = fmaf(w, y.z, o.z); o.w = fmaf(w, y.w, o.w);
+        }
+        return o;
+    };
+    auto put = [&](const KaPiece& pc, int r, int d, int head, const float4& o, bool final, size_t place) {   // place: of the scratch
+        const float2 ml = stat[r][head];
+        if (final) {
+            const float inv = ka_norm(ml.y), y[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+            ka_store(a, ka_out_at(a, pc.row0, pc.hk, pc.q0 + r, D) + d, y);
+        } else {
+            float* to = reinterpret_cast<float*>(a.part + place * S::SLOT) + r * S::PITCH;
+            __stcg(reinterpret_cast<float4*>(to + d), o);
+            if (d == 0) __stcg(reinterpret_cast<float2*>(to + D), ml);
+        }
+    };
+
+    // The warps' pieces.  One of an item that other CTAs have parts of goes to the scratch: place 0 if the item began in an earlier CTA, else
+    // place 1; the CTA has one of each at most.
+    const KaPiece mine = lane < 2 * W ? pieces[lane] : KaPiece{};
+    int open0, open1;   // a piece of the item at place 0, 1; -1: none
+    {
+        auto at = [&](int k) -> uint32_t { return pieces[k].at; };
+        const unsigned there = __ballot_sync(0xffffffffu, mine.nt != 0), below = there & ((1u << lane) - 1u);
+        const uint32_t before = __shfl_sync(0xffffffffu, mine.first, below ? 31 - __clz(below) : 0);
+        const bool head = mine.nt != 0 && (below == 0 || before != mine.first);
+        const unsigned heads = __ballot_sync(0xffffffffu, head);
+        const bool whole = mine.first >= c0 && mine.first + (uint32_t)mine.nt <= c1;
+        open0 = __ffs(__ballot_sync(0xffffffffu, head && !whole && mine.first < c0)) - 1;
+        open1 = __ffs(__ballot_sync(0xffffffffu, head && !whole && mine.first >= c0)) - 1;
+        if (warp == 0 && head) group_head[__popc(heads & ((1u << lane) - 1u))] = lane;
+        weigh(there, heads, mine.at, ROWS);
+        __syncthreads();
+        const int units = __popc(heads) * ROWS * (D / 4);
+        for (int i = threadIdx.x; i < units; i += W * 32) {
+            const int r = i / (D / 4) % ROWS, d = i % (D / 4) * 4, e = group_head[i / (ROWS * (D / 4))];
+            const KaPiece& pc = pieces[e];
+            if (r >= pc.rows - pc.q0) continue;
+            const unsigned later = heads & ~((2u << e) - 1u);
+            put(pc, r, d, e, sum_parts(there, e, later ? __ffs(later) - 1 : 2 * W, r, d, at), e != open0 && e != open1, (size_t)blockIdx.x * 4 + (e == open0 ? 0 : 1));
         }
     }
+    if (open0 < 0 && open1 < 0) return;   // (the same in all threads: every warp has looked at all pieces)
 
-    // ---- items that several CTAs share: the last one of a group to arrive merges the group ----------------------
-    for (int place = 0; place < 2; ++place) {
-        if (open[place].nt == 0) continue;   // (the same in all threads: every thread has walked all pieces)
-        const KaPiece pc = open[place];
-        const int rows = min(ROWS, pc.rows - pc.q0);
-        const int f = (int)(kv8_run_of(total, pc.start, n_run) / W), e = (int)(kv8_run_of(total, pc.start + (uint32_t)pc.nt - 1u, n_run) / W);
-        const int n = e - f + 1, group = kv8_merge_group(n);
-        const int f_place = pc.start <= kv8_run_begin(total, (uint32_t)f * W, n_run) ? 0 : 1;   // (only the first CTA's can be 1)
-        int my = (int)blockIdx.x - f;
-        // level 0: entries of my group; level 1: the groups' results, each at its first entry
-        for (int level = 0; level < 2; ++level) {
-            const int step = level == 0 ? 1 : group;
-            const int lo = level == 0 ? my / group * group : 0;
-            const int count = level == 0 ? min(group, n - lo) : (n + group - 1) / group;
-            if (level == 1 && count == 1) break;
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                unsigned* ticket = a.tickets + level * KA_MAX_CTAS * 2 + (f + lo) * 2 + (lo == 0 ? f_place : 0);
-                const bool last = atomicAdd(ticket, 1u) == (unsigned)count - 1u;
-                if (last) *ticket = 0u;   // (as the next call wants it: all have been here)
-                last_flag = last ? 1 : 0;
-            }
-            __syncthreads();
-            const bool go = last_flag != 0;
-            __syncthreads();
-            if (!go) break;
-            __threadfence();
-            const bool final = level == 1 || count == n;
-            float* s_acc = reinterpret_cast<float*>(smem);             // [W][ROWS][D]
-            float2* s_ml = reinterpret_cast<float2*>(smem + W * ROWS * D * 4);   // [count][ROWS]
-            auto entry = [&](int i) -> size_t {                        // row 0 of entry i
-                const int k = lo + i * step;
-                return ((size_t)(f + k) * 2 + (k == 0 ? f_place : 0)) * ROWS;
-            };
-            for (int i = threadIdx.x; i < count * ROWS; i += W * 32)
-                if (i % ROWS < rows) s_ml[i] = __ldcg(reinterpret_cast<const float2*>(a.ml) + entry(i / ROWS) + i % ROWS);
-            __syncthreads();
-            // each warp takes entries warp, warp + W, ... of all rows, four rows' loads in flight
-            for (int r0 = 0; r0 < rows; r0 += 4) {
-                float base[4], acc[4][NV];
+    // Items that several CTAs share: the last CTA of a group to arrive merges the group, the last group's the groups.  An item's entries:
+    // its first CTA's place 1, the others' place 0; a group's result: the group's first CTA's place 3 (the item's first CTA) or 2.
+    // A counter has two halves: a CTA can be the first of a group of an item that began earlier, and of an item that begins there.
+    for (int level = 0; level < 2; ++level) {
+        int lo[2] = {0, 0}, entries[2] = {0, 0}, step[2] = {1, 1}, f[2] = {0, 0};
+        bool final[2] = {false, false};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float top = -INFINITY;
-                    if (r0 + q < rows)
-                        for (int i = lane; i < count; i += 32) top = fmaxf(top, s_ml[i * ROWS + r0 + q].x);
-#pragma unroll
-                    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    base[q] = top == -INFINITY ? 0.f : top;
-#pragma unroll
-                    for (int v = 0; v < NV; ++v) acc[q][v] = 0.f;
-                }
-                for (int i = warp; i < count; i += W) {
-                    const size_t at = entry(i);
-                    float2 y[4][NV / 2];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-#pragma unroll
-                        for (int v = 0; v < NV / 2; ++v)
-                            y[q][v] = r0 + q < rows ? __ldcg(reinterpret_cast<const float2*>(a.part + (at + r0 + q) * D + NV * lane) + v) : make_float2(0.f, 0.f);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (r0 + q >= rows) continue;
-                        const float w = ka_exp2(s_ml[i * ROWS + r0 + q].x - base[q]);
-#pragma unroll
-                        for (int v = 0; v < NV / 2; ++v) {
-                            acc[q][2 * v] = fmaf(w, y[q][v].x, acc[q][2 * v]);
-                            acc[q][2 * v + 1] = fmaf(w, y[q][v].y, acc[q][2 * v + 1]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (r0 + q < rows) {
-#pragma unroll
-                        for (int v = 0; v < NV; v += 2)
-                            *reinterpret_cast<float2*>(s_acc + ((size_t)warp * ROWS + r0 + q) * D + NV * lane + v) = make_float2(acc[q][v], acc[q][v + 1]);
-                    }
-            }
-            __syncthreads();
-            for (int r = warp; r < rows; r += W) {
-                float top = -INFINITY, ls = 0.f, acc[NV];
-                for (int i = lane; i < count; i += 32) top = fmaxf(top, s_ml[i * ROWS + r].x);
-#pragma unroll
-                for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const float base = top == -INFINITY ? 0.f : top;
-                for (int i = 0; i < count; ++i) ls = fmaf(ka_exp2(s_ml[i * ROWS + r].x - base), s_ml[i * ROWS + r].y, ls);
-#pragma unroll
-                for (int v = 0; v < NV; ++v) acc[v] = 0.f;
-                for (int w = 0; w < min(W, count); ++w)
-#pragma unroll
-                    for (int v = 0; v < NV; ++v) acc[v] += s_acc[((size_t)w * ROWS + r) * D + NV * lane + v];
-                if (final) {
-                    const float inv = ka_norm(ls);
-#pragma unroll
-                    for (int v = 0; v < NV; ++v) acc[v] *= inv;
-                    ka_store(a, ka_out_at(a, pc.row0, pc.hk, pc.q0 + r, D) + NV * lane, acc);
-                } else {
-                    const size_t at = entry(0) + r;
-#pragma unroll
-                    for (int v = 0; v < NV; v += 2) __stcg(reinterpret_cast<float2*>(a.part + at * D + NV * lane + v), make_float2(acc[v], acc[v + 1]));
-                    if (lane == 0) __stcg(reinterpret_cast<float2*>(a.ml) + at, make_float2(top, ls));
-                }
-            }
-            if (final) break;
-            my = lo;   // (this CTA goes on for its group)
+        for (int k = 0; k < 2; ++k) {
+            const int e = k == 0 ? open0 : open1;
+            if (e < 0) continue;
+            const uint32_t first = pieces[e].first;
+            f[k] = (int)kv8_cta_of(cut, first);
+            const int n = (int)kv8_cta_of(cut, first + (uint32_t)pieces[e].nt - 1u) - f[k] + 1, group = kv8_merge_group(n);
+            lo[k] = level == 0 ? ((int)blockIdx.x - f[k]) / group * group : 0;
+            entries[k] = level == 0 ? min(group, n - lo[k]) : (n + group - 1) / group;
+            step[k] = level == 0 ? 1 : group;
+            final[k] = level == 1 || entries[k] == n;
         }
-        __syncthreads();   // (the next place's merge uses the same shared memory)
+        __syncthreads();   // (this CTA's parts are written)
+        if (threadIdx.x < 2) {
+            const int k = threadIdx.x, l = k == 0 ? lo[0] : lo[1], n = k == 0 ? entries[0] : entries[1];
+            bool last = false;
+            if (n > 0) last = ka_arrive(a.tickets + level * KA_MAX_CTAS + (k == 0 ? f[0] : f[1]) + l, l > 0 ? 0x10000u : 1u, (unsigned)n);
+            last_flag[k] = last ? 1 : 0;
+        }
+        __syncthreads();
+        bool more = false;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const int n = k == 0 ? entries[0] : entries[1];
+            if (n == 0 || !last_flag[k]) {
+                if (k == 0) open0 = -1; else open1 = -1;
+                continue;
+            }
+            const KaPiece pc = pieces[k == 0 ? open0 : open1];
+            const int base = k == 0 ? f[0] : f[1], l = k == 0 ? lo[0] : lo[1], st = k == 0 ? step[0] : step[1];
+            const bool fin = k == 0 ? final[0] : final[1];
+            const int rows = min(ROWS, pc.rows - pc.q0), pieces16 = rows * S::PITCH / 4;   // 16-byte pieces of an entry
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem);
+            for (int e = warp; e < n; e += W) {
+                const int c = l + e * st;
+                const uint8_t* src = a.part + ((size_t)(base + c) * 4 + (level == 1 ? 2 : 0) + (c == 0 ? 1 : 0)) * S::SLOT;
+#pragma unroll 4
+                for (int i = lane; i < pieces16; i += 32) ka_cp16(dst + e * S::SLOT + i * 16, src + i * 16);
+            }
+            ka_commit();
+            ka_wait<0>();
+            __syncthreads();
+            auto at = [](int e) -> uint32_t { return (uint32_t)(e * S::SLOT); };
+            const unsigned there = (1u << n) - 1u;
+            weigh(there, 1u, at(min(lane, n - 1)), rows);
+            __syncthreads();
+            for (int i = threadIdx.x; i < rows * (D / 4); i += W * 32) {
+                const int r = i / (D / 4), d = i % (D / 4) * 4;
+                put(pc, r, d, 0, sum_parts(there, 0, n, r, d, at), fin, (size_t)(base + l) * 4 + (l == 0 ? 3 : 2));
+            }
+            if (fin) { if (k == 0) open0 = -1; else open1 = -1; }
+            else more = true;
+            __syncthreads();   // (the next merge uses the same shared memory)
+        }
+        if (!more) return;
     }
 }
 
-template <int D, int NT>
+template <int D, int QT>
 static cudaError_t launch_ka(const KaArgs& a, cudaStream_t s) {
-    using S = KaShape<D, NT>;
+    using S = KaShape<D, QT>;
     static PerDeviceOnce configured;
     const int rc = configured.run(current_device(), [] {
-        return (int)cudaFuncSetAttribute(kv8_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+        return (int)cudaFuncSetAttribute(kv8_attn_kernel<D, QT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     });
     if (rc != 0) return rc < 0 ? cudaErrorInvalidDevice : (cudaError_t)rc;
     const int grid = sm_count() < KA_MAX_CTAS ? sm_count() : KA_MAX_CTAS;
-    const cudaError_t e = launch_pdl(kv8_attn_kernel<D, NT>, dim3((unsigned)grid), dim3(S::WARPS * 32), S::SMEM, s, a);
+    const cudaError_t e = launch_pdl(kv8_attn_kernel<D, QT>, dim3((unsigned)grid), dim3(S::WARPS * 32), S::SMEM, s, a);
     count_launch();
     return e;
 }
@@ -699,17 +780,27 @@ cudaError_t launch_kv8_attn(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, co
     a.B = b.n_seqs; a.T = T; a.n_each = T / b.n_seqs; a.Hkv = c.n_kv_heads; a.G = n_heads / c.n_kv_heads;
     a.shift = 0;
     while ((AQ_KV8_BLOCK << a.shift) < c.page) ++a.shift;
+    a.G_magic = kv8_magic((uint32_t)a.G);
     a.q_bf16 = dt == AQ_BF16; a.out_dtype = (int)out_dt;
     a.scale_log2 = scale * 1.4426950408889634f;
     uint8_t* sc = reinterpret_cast<uint8_t*>(scratch);
     a.tickets = reinterpret_cast<unsigned*>(sc);
-    a.ml = reinterpret_cast<float*>(sc + KA_TICKET_BYTES);
-    a.part = reinterpret_cast<float*>(sc + KA_TICKET_BYTES + KA_ML_BYTES);
-    // sixteen query rows per pass over a request's keys and values where it has more than eight, on average
-    const bool wide = (int64_t)a.G * T > 8 * (int64_t)a.B;
-    if (c.head_dim == 64) return wide ? launch_ka<64, 2>(a, s) : launch_ka<64, 1>(a, s);
-    if (c.head_dim == 128) return wide ? launch_ka<128, 2>(a, s) : launch_ka<128, 1>(a, s);
-    return launch_ka<256, 1>(a, s);
+    a.part = sc + KA_TICKET_BYTES;
+    // query rows per pass over a request's keys and values: what it has of them on average
+    const int64_t rows = ((int64_t)a.G * T + a.B - 1) / a.B;
+    const int qt = rows <= 4 ? 1 : rows <= 8 || c.head_dim == 256 ? 2 : rows <= 12 ? 3 : 4;
+    switch (c.head_dim + qt) {
+        case 65: return launch_ka<64, 1>(a, s);
+        case 66: return launch_ka<64, 2>(a, s);
+        case 67: return launch_ka<64, 3>(a, s);
+        case 68: return launch_ka<64, 4>(a, s);
+        case 129: return launch_ka<128, 1>(a, s);
+        case 130: return launch_ka<128, 2>(a, s);
+        case 131: return launch_ka<128, 3>(a, s);
+        case 132: return launch_ka<128, 4>(a, s);
+        case 257: return launch_ka<256, 1>(a, s);
+        default: return launch_ka<256, 2>(a, s);
+    }
 }
 
 }  // namespace aq

@@ -1,9 +1,9 @@
 // How the attention over the paged 8-bit cache is dealt to CTAs and warps, and which rows of a step belong to which request: the
 // index arithmetic of aq_kv8.cu and aq_kv8_attn.cu.  Plain C++ (host and device), so it can be unit-tested without a GPU.
 //
-// The work is a line of tiles of 32 positions: requests in order, within a request (key/value head, block of query rows), within
-// such an item its tiles.  The line is cut into one contiguous run per warp, equal to within a tile; neighbouring warps of a CTA
-// hold neighbouring runs.
+// The work is a line: requests in order, within a request its items (key/value head, block of query rows), of each item first
+// KV8_ITEM_COST places for what an item costs beside its tiles (queries in, output out), then its tiles of 32 positions.  The line is
+// cut into one contiguous run per warp, equal to within one place; neighbouring warps of a CTA hold neighbouring runs.
 #pragma once
 #include <cstdint>
 
@@ -15,11 +15,35 @@
 
 namespace aq {
 
-// First tile of run i of n runs over `total` tiles (i == n: the end).
-AQ_HD uint32_t kv8_run_begin(uint32_t total, uint32_t i, uint32_t n) { return (uint32_t)((uint64_t)total * i / n); }
+constexpr uint32_t KV8_ITEM_COST = 1;
 
-// The run that holds tile x (x < total): the last one that begins at or before it.
-AQ_HD uint32_t kv8_run_of(uint32_t total, uint32_t x, uint32_t n) { return (uint32_t)(((uint64_t)(x + 1u) * n - 1u) / total); }
+// CTAs of a launch over a line of `total` places with `items` items, `warps` warps each, at most `most`.  Where there is a CTA for
+// every item and its warps have few tiles of it (five places), one each: nothing is then merged between CTAs, which costs a chain
+// of trips to memory (32 items of 16 tiles: 12.2 us with two CTAs per item).  Else a place per warp at least.
+AQ_HD uint32_t kv8_ctas(uint32_t total, uint32_t items, uint32_t warps, uint32_t most) {
+    if (items <= most && total <= items * warps * 5u) return items;
+    const uint32_t n = (total + warps - 1u) / warps;
+    return n < most ? n : most;
+}
+
+// How a line of `total` places is cut into `n` CTAs' shares (1 <= n <= total): the first `more` have one place more than the others.  One
+// division for the cut and one per look-up; a 64-bit quotient here was a microsecond of every small call.
+struct Kv8Cut { uint32_t each, more; };
+AQ_HD Kv8Cut kv8_cut(uint32_t total, uint32_t n) {
+    const uint32_t q = total / n;
+    return Kv8Cut{q, total - q * n};
+}
+AQ_HD uint32_t kv8_begin(const Kv8Cut& c, uint32_t i) { return c.each * i + (i < c.more ? i : c.more); }   // (i == n: the end)
+AQ_HD uint32_t kv8_cta_of(const Kv8Cut& c, uint32_t x) {
+    const uint32_t longer = c.more * (c.each + 1u);
+    return x < longer ? x / (c.each + 1u) : c.more + (x - longer) / c.each;
+}
+// First place of warp w of W in a CTA's share [a, e).
+AQ_HD uint32_t kv8_warp_begin(uint32_t a, uint32_t e, uint32_t w, uint32_t W) { return a + (uint32_t)((uint64_t)(e - a) * w / W); }
+
+// x / d for a divisor that the host knows: m = kv8_magic(d), exact for x * d < 2^32 (d > 1).
+AQ_HD uint32_t kv8_magic(uint32_t d) { return d == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / d) + 1u; }
+AQ_HD uint32_t kv8_div(uint32_t x, uint32_t m) { return m == 0u ? x : (uint32_t)((uint64_t)x * m >> 32); }
 
 // Rows of request b in a step of T rows: row_start as the caller gave it, held inside the step whatever it says.
 struct Kv8Rows { int first, n; };
@@ -43,7 +67,7 @@ AQ_HD int kv8_find(const T* begin, int n, T x) {
 // Partial results of an item that n CTAs share are merged in groups of this many, then the groups' results: what one CTA reads
 // grows with the square root of n.
 AQ_HD int kv8_merge_group(int n) {
-    if (n <= 16) return n;
+    if (n <= 14) return n;
     int g = 4;
     while (g * g < n) ++g;
     return g;

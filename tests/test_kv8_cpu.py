@@ -148,37 +148,44 @@ SRC = textwrap.dedent(r"""
     using namespace aq;
     #define CHECK(c) do { if (!(c)) { std::printf("FAIL line %d: %s\n", __LINE__, #c); return 1; } } while (0)
     int main() {
-        // every tile belongs to the run that run_of says, runs differ by one tile at most
+        // every place belongs to the share that cta_of says, shares differ by one place at most, warps' runs too
         for (uint32_t total : {1u, 2u, 7u, 8u, 9u, 63u, 64u, 511u, 1183u, 1184u, 1185u, 5000u})
-            for (uint32_t n : {1u, 2u, 8u, 16u, 24u, 148u, 592u, 1184u}) {
-                uint32_t lo = 0xffffffffu, hi = 0;
-                CHECK(kv8_run_begin(total, 0, n) == 0 && kv8_run_begin(total, n, n) == total);
+            for (uint32_t n : {1u, 2u, 8u, 16u, 24u, 147u, 148u}) {
+                if (n > total) continue;
+                const Kv8Cut cut = kv8_cut(total, n);
+                CHECK(kv8_begin(cut, 0) == 0 && kv8_begin(cut, n) == total);
                 for (uint32_t i = 0; i < n; ++i) {
-                    const uint32_t a = kv8_run_begin(total, i, n), b = kv8_run_begin(total, i + 1, n);
-                    CHECK(a <= b);
-                    if (b - a < lo) lo = b - a;
-                    if (b - a > hi) hi = b - a;
-                    for (uint32_t x = a; x < b; ++x) CHECK(kv8_run_of(total, x, n) == i);
+                    const uint32_t a = kv8_begin(cut, i), e = kv8_begin(cut, i + 1);
+                    CHECK(e - a == total / n || e - a == (total + n - 1) / n);
+                    CHECK(e > a);
+                    for (uint32_t x = a; x < e; ++x) CHECK(kv8_cta_of(cut, x) == i);
+                    for (uint32_t W : {4u, 8u, 16u}) {
+                        CHECK(kv8_warp_begin(a, e, 0, W) == a && kv8_warp_begin(a, e, W, W) == e);
+                        for (uint32_t w = 0; w < W; ++w) {
+                            const uint32_t len = kv8_warp_begin(a, e, w + 1, W) - kv8_warp_begin(a, e, w, W);
+                            CHECK(len == (e - a) / W || len == (e - a + W - 1) / W);
+                        }
+                    }
                 }
-                CHECK(hi - lo <= 1);
             }
-        // counts near 2^32
-        const uint32_t big = 0xfffffff0u;
-        for (uint32_t i : {0u, 1u, 700u, 1183u}) {
-            const uint32_t a = kv8_run_begin(big, i, 1184), b = kv8_run_begin(big, i + 1, 1184);
-            CHECK(a < b && kv8_run_of(big, a, 1184) == i && kv8_run_of(big, b - 1, 1184) == i);
+        // counts near 2^31
+        const uint32_t big = 0x7ffffff0u;
+        const Kv8Cut cut = kv8_cut(big, 148);
+        CHECK(kv8_begin(cut, 148) == big);
+        for (uint32_t i : {0u, 1u, 70u, 147u}) {
+            const uint32_t a = kv8_begin(cut, i), e = kv8_begin(cut, i + 1);
+            CHECK(a < e && kv8_cta_of(cut, a) == i && kv8_cta_of(cut, e - 1) == i && kv8_warp_begin(a, e, 15, 16) < e);
         }
-        CHECK(kv8_run_begin(big, 1184, 1184) == big);
-        // a CTA's range is the union of its warps' runs, and with ceil(total / warps) CTAs none is empty
-        for (uint32_t W : {4u, 8u})
-            for (uint32_t total = 1; total < 3000; ++total) {
-                const uint32_t ctas = (total + W - 1) / W < 148 ? (total + W - 1) / W : 148;
-                for (uint32_t c = 0; c < ctas; ++c) {
-                    const uint32_t a = kv8_run_begin(total, c * W, ctas * W), b = kv8_run_begin(total, (c + 1) * W, ctas * W);
-                    CHECK(a < b);
-                    CHECK(kv8_run_of(total, a, ctas * W) / W == c && kv8_run_of(total, b - 1, ctas * W) / W == c);
+        // a launch has no CTA without a place: at least two places per item
+        for (uint32_t W : {4u, 8u, 16u})
+            for (uint32_t total = 2; total < 3000; ++total)
+                for (uint32_t items : {1u, (total + 5) / 7, total / 2}) {
+                    const uint32_t ctas = kv8_ctas(total, items, W, 148);
+                    CHECK(ctas >= 1 && ctas <= 148 && ctas <= total);
                 }
-            }
+        for (uint32_t d = 1; d <= 256; ++d)
+            for (uint32_t x : {0u, 1u, d - 1, d, d + 1, 7 * d - 1, 7 * d, 4095 * d, 4096 * d - 1, 4096 * d})
+                CHECK(kv8_div(x, kv8_magic(d)) == x / d);
         // rows of a step whatever the caller's array says
         CHECK(kv8_rows(3, 7, 10).first == 3 && kv8_rows(3, 7, 10).n == 4);
         CHECK(kv8_rows(7, 3, 10).n == 0 && kv8_rows(-5, 3, 10).first == 0 && kv8_rows(-5, 3, 10).n == 3);
@@ -190,7 +197,7 @@ SRC = textwrap.dedent(r"""
         // merge groups cover all entries with few reads
         for (int n = 1; n <= 192; ++n) {
             const int g = kv8_merge_group(n), groups = (n + g - 1) / g;
-            CHECK(g >= 1 && g <= 16 && groups <= 16 && (n <= 16) == (groups == 1));
+            CHECK(g >= 1 && g <= 14 && groups <= 14 && (n <= 14) == (groups == 1));
         }
         std::printf("ok\n");
         return 0;
