@@ -305,7 +305,7 @@ aq_status_t aq_rope_setup(int rot_dim, int layout, double theta, int scaling, do
  *   out_dev: DEVICE, likewise of out_dtype (= dtype, or a half type for AQ_F32 input), out_stride apart; may be x_dev itself with the same
  *            type and stride (in place), else no element of the one may be one of the other
  *   pos_dev: DEVICE int32 [n_rows]; rows with a negative position are left as they are
- * head_dim >= 2; n_rows * n_heads < 2^31; element alignment suffices (16-byte aligned rows with multiples of 8 or 16 elements run eight at a time).
+ * head_dim 2 .. 1024, n_heads 1 .. 4096, n_rows * n_heads < 2^31; element alignment suffices (16-byte aligned rows with multiples of 8 or 16 elements run eight at a time).
  * Queries and keys of a fused projection rotate in one call: they are neighbouring heads of a row.
  */
 aq_status_t aq_rope_rows(const aq_rope_t* rope, const void* x_dev, aq_dtype_t dtype, int64_t x_stride, void* out_dev, aq_dtype_t out_dtype,

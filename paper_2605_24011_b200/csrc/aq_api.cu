@@ -568,9 +568,8 @@ aq_status_t aq_rope_rows(const aq_rope_t* rope, const void* x_dev, aq_dtype_t dt
     if (reinterpret_cast<uintptr_t>(x_dev) % in_size || reinterpret_cast<uintptr_t>(out_dev) % out_size) return AQ_ERR_INVALID_ARG;
     if (rope->rot_dim < 2 || (rope->rot_dim & 1) || rope->rot_dim > 2 * AQ_ROPE_MAX_PAIRS || (rope->layout != AQ_ROPE_HALF && rope->layout != AQ_ROPE_PAIRS))
         return AQ_ERR_INVALID_ARG;
-    if (n_rows < 1 || n_heads < 1 || head_dim < 2 || head_dim > (1 << 16) || n_heads > (1 << 16) || rope->rot_dim > head_dim ||
-        n_rows >= ((int64_t)1 << 31) / n_heads)
-        return AQ_ERR_INVALID_ARG;
+    if (n_rows < 1 || n_heads < 1 || head_dim < 2 || rope->rot_dim > head_dim || n_rows >= ((int64_t)1 << 31) / n_heads) return AQ_ERR_INVALID_ARG;
+    if (head_dim > 1024 || n_heads > 4096) return AQ_ERR_UNSUPPORTED;
     const int64_t row = (int64_t)n_heads * head_dim, most = (int64_t)1 << 40;
     if (x_stride < row || out_stride < row || x_stride > most || out_stride > most) return AQ_ERR_INVALID_ARG;
     if (x_dev == out_dev && (dtype != out_dtype || x_stride != out_stride)) return AQ_ERR_INVALID_ARG;

@@ -80,12 +80,28 @@ __device__ __forceinline__ void kp_scan3(int (&v)[3], int (&tot)[3], int (*sums)
     }
 }
 
+// put(lane's request, j) for j < n: the first FEW by the request's own thread (most requests have one or none), the rest by its warp, 32 at a
+// time.  (A search for the request of each row instead: 4096 rows and 3500 pages of 1000 requests 6.7 us, 8.3 with four searches at once.)
+template <int FEW, typename Fn>
+__device__ __forceinline__ void kp_each(int n, Fn put) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < FEW; ++j)
+        if (j < n) put(lane, j);
+    for (unsigned left = __ballot_sync(0xffffffffu, n > FEW); left; left &= left - 1) {
+        const int src = __ffs(left) - 1, m = __shfl_sync(0xffffffffu, n, src);
+#pragma unroll 4
+        for (int j = FEW + lane; j < m; j += 32) put(src, j);
+    }
+}
+
 __global__ void __launch_bounds__(KP_THREADS, 1) kv8_plan_kernel(const KpArgs a) {
     __shared__ int sums[33][3];
-    __shared__ int back_at[AQ_KV8_MAX_SEQS + 1], take_at[AQ_KV8_MAX_SEQS + 1], row_at[AQ_KV8_MAX_SEQS + 1];
-    __shared__ int s_len[AQ_KV8_MAX_SEQS], s_held[AQ_KV8_MAX_SEQS];
+    __shared__ int4 of[KP_THREADS];   // of a request: where its given pages go, where its taken ones come from, its first row; pages held
+    __shared__ int length[KP_THREADS];
     const int b = threadIdx.x, P = 1 << a.shift;
     pdl_wait();
+    pdl_launch_dependents();
     const int n_free = __ldg(a.n_free);
     int len = 0, add = 0;
     if (b < a.B) { len = __ldg(a.lens + b); add = __ldg(a.added + b); }
@@ -96,11 +112,8 @@ __global__ void __launch_bounds__(KP_THREADS, 1) kv8_plan_kernel(const KpArgs a)
     const int grown = ok && add >= 0 ? (int)(((int64_t)len + add + P - 1) >> a.shift) - held : 0;
     int v[3] = {ok && add < 0 ? held : 0, grown, ok ? max(add, 0) : 0}, tot[3];
     kp_scan3(v, tot, sums);
-    if (b < a.B) {
-        back_at[b] = v[0]; take_at[b] = v[1]; row_at[b] = v[2];
-        s_len[b] = len; s_held[b] = held;
-    }
-    if (b == 0) { back_at[a.B] = tot[0]; take_at[a.B] = tot[1]; row_at[a.B] = tot[2]; }
+    of[b] = make_int4(v[0], v[1], v[2], held);   // (read by the warp itself)
+    length[b] = len;
     ok = ok && tot[2] <= a.n_rows && n_free >= 0 && (int64_t)n_free + tot[0] <= a.free_cap && (int64_t)tot[1] <= (int64_t)n_free + tot[0];
     ok = __syncthreads_and(ok);
     if (!ok) {   // nothing changes, and the step has no rows
@@ -111,28 +124,25 @@ __global__ void __launch_bounds__(KP_THREADS, 1) kv8_plan_kernel(const KpArgs a)
         for (int i = b; i < a.n_rows; i += KP_THREADS) a.pos[i] = -1;
         return;
     }
+    const int b0 = b & ~31;   // the warp's first request
     // pages of ended requests go on the stack, in the order of the requests and their pages
-    for (int i = b; i < tot[0]; i += KP_THREADS) {
-        const int r = kv8_find(back_at, a.B, i);
-        a.free_list[n_free + i] = a.table[(int64_t)r * a.width + (i - back_at[r])];
+    kp_each<0>(add < 0 ? held : 0, [&](int k, int j) { a.free_list[n_free + of[b0 + k].x + j] = __ldg(a.table + (int64_t)(b0 + k) * a.width + j); });
+    if (b < a.B) {
+        a.lens_out[b] = add < 0 ? 0 : len + add;
+        a.row_start[b] = v[2];
     }
-    if (b < a.B) a.lens_out[b] = add < 0 ? 0 : len + add;
-    if (b == 0) *a.n_free_out = n_free + tot[0] - tot[1];
-    for (int i = b; i <= a.B; i += KP_THREADS) a.row_start[i] = row_at[i];
-    for (int i = b; i < a.n_rows; i += KP_THREADS) {
-        int p = -1;
-        if (i < tot[2]) {
-            const int r = kv8_find(row_at, a.B, i);
-            p = s_len[r] + i - row_at[r];
-        }
-        a.pos[i] = p;
+    if (b == 0) {
+        *a.n_free_out = n_free + tot[0] - tot[1];
+        a.row_start[a.B] = tot[2];
     }
+    kp_each<1>(max(add, 0), [&](int k, int j) { a.pos[of[b0 + k].z + j] = length[b0 + k] + j; });
+    for (int i = tot[2] + b; i < a.n_rows; i += KP_THREADS) a.pos[i] = -1;
     __syncthreads();   // (pages that have just been given back may be taken)
     // requests that grow take theirs from the top, in the same order
-    for (int i = b; i < tot[1]; i += KP_THREADS) {
-        const int r = kv8_find(take_at, a.B, i);
-        a.table[(int64_t)r * a.width + s_held[r] + (i - take_at[r])] = a.free_list[n_free + tot[0] - 1 - i];
-    }
+    kp_each<1>(grown, [&](int k, int j) {
+        const int4 f = of[b0 + k];
+        a.table[(int64_t)(b0 + k) * a.width + f.w + j] = a.free_list[n_free + tot[0] - 1 - f.y - j];
+    });
 }
 
 cudaError_t launch_kv8_plan(const int32_t* lens, const int32_t* added, int n_seqs, int page, int32_t* table, int64_t width, int32_t* free_list,
@@ -149,8 +159,8 @@ cudaError_t launch_kv8_plan(const int32_t* lens, const int32_t* added, int n_seq
 }
 
 // ---- append ---------------------------------------------------------------------------------------------------
-// A unit of work is what a step brings to one block of 32 positions of one head, keys or values: up to 32 rows that one warp
-// holds in registers, so they are read once:
+// A unit of work is what a step brings to one block of 32 positions of one head, keys or values: up to 32 rows that its warps
+// hold in registers, so they are read once:
 //     need = up11(max |x| / 127),  s = need <= s_old ? s_old : max(need, up11(1.25 s_old)),  code = rint(x / s)
 // up11: the next binary32 value of 11 significant bits.  With both x (11 bits at most) and s that short, the binary32 quotient
 // is at a half exactly where the true one is, so the rounding is the true quotient's.  A block whose first position is among the
@@ -173,12 +183,23 @@ constexpr int KW_WARPS = 4;
 
 __device__ __forceinline__ float kw_up11(float x) { return __uint_as_float((__float_as_uint(x) + 0x1FFFu) & ~0x1FFFu); }
 
-template <int D, bool BF16>
-__device__ __forceinline__ void kw_unit(const uint16_t* x, int64_t x_row, int n, int at, uint8_t* codes, float* scale) {
-    constexpr int LPR = D / 8;          // lanes per row (16 bytes each)
-    constexpr int RPP = 32 / LPR;       // rows per pass
-    constexpr int NV = 32 / RPP;        // passes of a whole block
-    const int lane = threadIdx.x & 31, sub = lane / LPR, c = lane % LPR;
+// rint(x / s) for |x / s| < 2^21 as the low bits of a float: the quotient correctly rounded (x inv, corrected by its exact remainder),
+// then rounded to a whole number by adding 1.5 * 2^23.  inv = 1 / s rounded; s in 2^-60 .. 2^125.
+__device__ __forceinline__ uint32_t kw_quotient(float x, float s, float inv) {
+    const float q = x * inv;
+    return __float_as_uint(fmaf(fmaf(-q, s, x), inv, q) + 12582912.f);
+}
+__device__ __forceinline__ uint32_t kw_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {   // their low bytes
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+// WPU warps of a unit (1, or the CTA's 4, all of which call this together): w is this one's number among them.
+template <int D, bool BF16, int WPU>
+__device__ __forceinline__ void kw_unit(const uint16_t* x, int64_t x_row, int n, int at, uint8_t* codes, float* scale, int w, uint32_t* meet) {
+    constexpr int LPR = D / 8;                // lanes per row (16 bytes each)
+    constexpr int RPP = 32 / LPR * WPU;       // rows per pass
+    constexpr int NV = 32 / RPP;              // passes of a whole block
+    const int lane = threadIdx.x & 31, sub = w * (32 / LPR) + lane / LPR, c = lane % LPR;
     uint4 v[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -190,63 +211,89 @@ __device__ __forceinline__ void kw_unit(const uint16_t* x, int64_t x_row, int n,
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) most = __vmaxu2(most, w[k] & 0x7fff7fffu);
+        for (int k = 0; k < 4; ++k) most = __vmaxu2(most, u[k] & 0x7fff7fffu);
     }
+    most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
+    if constexpr (WPU > 1) {
+        if (lane == 0) meet[w] = most;
+        __syncthreads();                      // (and every warp has read the scale)
 #pragma unroll
-    for (int d = 16; d; d >>= 1) most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, d));
-    const uint32_t big = max(most & 0xffffu, most >> 16);
+        for (int k = 0; k < WPU; ++k) most = max(most, meet[k]);
+        __syncthreads();
+    }
     auto wide = [](uint32_t h) -> float {
         if constexpr (BF16) return __uint_as_float(h << 16);
         else return __half2float(__ushort_as_half((unsigned short)h));
     };
-    const bool poison = big >= (BF16 ? 0x7f80u : 0x7c00u) || !(s_old == s_old);
-    const float need = kw_up11(wide(big) / 127.f);
+    const bool poison = most >= (BF16 ? 0x7f80u : 0x7c00u) || !(s_old == s_old);
+    const float need = kw_up11(wide(most) / 127.f);
     float s = need <= s_old ? s_old : fmaxf(need, kw_up11(1.25f * s_old));
     if (poison) s = __uint_as_float(0x7fc00000u);
-    const float fit = s > 0.f ? s : 1.f;   // (0: a block of zeros; NaN: the codes do not matter, they become 0)
-    auto code = [&](uint32_t h) -> uint32_t {
-        const float q = rintf(__fdiv_rn(wide(h), fit));
-        return poison ? 0u : (uint32_t)(int)q & 0xffu;
+    // A scale under 2^-60 (bfloat16 only) has no reciprocal to work with: both sides of the quotient times 2^100 then.  s = 0 is a block of
+    // zeros; of a NaN the codes do not matter, they become 0.
+    const float lift = s < 8.67361737988403547e-19f ? 1.2676506002282294e30f : 1.f;
+    const float fit = s > 0.f ? s * lift : 1.f, inv = poison ? 0.f : 1.f / fit;
+    auto pair = [&](uint32_t u, uint32_t& a, uint32_t& b) {
+        float e, f;
+        if constexpr (BF16) { e = __uint_as_float(u << 16); f = __uint_as_float(u & 0xffff0000u); }
+        else {
+            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&u));
+            e = h.x; f = h.y;
+        }
+        if (BF16 && lift != 1.f) { e *= lift; f *= lift; }
+        a = kw_quotient(e, fit, inv);
+        b = kw_quotient(f, fit, inv);
     };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int r = i * RPP + sub;
         if (r < n) {
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
             uint32_t o[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                o[k] = code(w[2 * k] & 0xffffu) | code(w[2 * k] >> 16) << 8 | code(w[2 * k + 1] & 0xffffu) << 16 | code(w[2 * k + 1] >> 16) << 24;
+            for (int k = 0; k < 2; ++k) {
+                uint32_t a, b, e, f;
+                pair(u[2 * k], a, b);
+                pair(u[2 * k + 1], e, f);
+                o[k] = poison ? 0u : kw_bytes(a, b, e, f);
+            }
             *reinterpret_cast<uint2*>(codes + (at + r) * D + 8 * c) = make_uint2(o[0], o[1]);
         }
     }
     if (s > s_old && at > 0 && !poison) {   // the older positions' codes on the larger scale
+        const float was_fit = s_old * lift;
         for (int r = sub; r < at; r += RPP) {
             uint2* p = reinterpret_cast<uint2*>(codes + r * D + 8 * c);
             const uint2 u = *p;
-            uint32_t o[2] = {0u, 0u};
+            uint32_t o[2];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int was = (int)(int8_t)((k < 4 ? u.x : u.y) >> (8 * (k & 3)));
-                const uint32_t now = (uint32_t)(int)rintf(__fdiv_rn((float)was * s_old, s)) & 0xffu;
-                o[k >> 2] |= now << (8 * (k & 3));
+            for (int h = 0; h < 2; ++h) {
+                uint32_t b[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) b[k] = kw_quotient((float)(int)(int8_t)((h ? u.y : u.x) >> (8 * k)) * was_fit, fit, inv);
+                o[h] = kw_bytes(b[0], b[1], b[2], b[3]);
             }
             *p = make_uint2(o[0], o[1]);
         }
     }
-    __syncwarp();   // (every lane has read the scale)
-    if (lane == 0 && (at == 0 || !(s == s_old))) *scale = s;
+    if constexpr (WPU == 1) __syncwarp();   // (every lane has read the scale)
+    if (w == 0 && lane == 0 && (at == 0 || !(s == s_old))) *scale = s;
 }
 
-template <int D, bool BF16>
+// WPU 1: a warp per unit, two heads' keys and values per CTA (decode steps: units of a row or a few).  WPU 4: the CTA's warps share each
+// unit, a head's keys or values per CTA (prompts: one warp per unit left an SM with a few thousand instructions in a row, 9 requests'
+// chunks of 333 rows of one head of 256 took 14.0 us).
+template <int D, bool BF16, int WPU>
 __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_constant__ KwArgs a) {
     __shared__ int begin[AQ_KV8_MAX_SEQS + 1];
+    __shared__ uint32_t meet[KW_WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int kv = warp & 1, hk = 2 * blockIdx.y + (warp >> 1);   // two heads' keys and values per CTA
+    const int kv = WPU == 1 ? warp & 1 : (int)blockIdx.z, hk = WPU == 1 ? 2 * blockIdx.y + (warp >> 1) : (int)blockIdx.y;
     const int t0 = blockIdx.x * a.chunk;
     pdl_wait();
+    pdl_launch_dependents();
     if (a.row_start) {
         for (int i = threadIdx.x; i <= a.B; i += KW_WARPS * 32) begin[i] = __ldg(a.row_start + i);
         __syncthreads();
@@ -284,13 +331,27 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_
             }
         }
     }
-    for (unsigned leaders = __ballot_sync(0xffffffffu, n > 0); leaders; leaders &= leaders - 1) {
+    for (unsigned leaders = __ballot_sync(0xffffffffu, n > 0); leaders; leaders &= leaders - 1) {   // (with WPU 4 the same in every warp)
         const int src = __ffs(leaders) - 1;
         const int u_at = __shfl_sync(0xffffffffu, at, src), u_n = __shfl_sync(0xffffffffu, n, src);
         const int64_t u_blk = __shfl_sync(0xffffffffu, blk, src);
-        kw_unit<D, BF16>(a.x[kv] + (int64_t)(t0 + src) * a.x_row + (int64_t)hk * D, a.x_row, u_n, u_at, a.codes[kv] + u_blk * AQ_KV8_BLOCK * D,
-                         a.scales[kv] + u_blk);
+        kw_unit<D, BF16, WPU>(a.x[kv] + (int64_t)(t0 + src) * a.x_row + (int64_t)hk * D, a.x_row, u_n, u_at, a.codes[kv] + u_blk * AQ_KV8_BLOCK * D,
+                              a.scales[kv] + u_blk, WPU == 1 ? 0 : warp, meet);
     }
+}
+
+template <int D, bool BF16>
+static cudaError_t launch_kw(KwArgs& a, cudaStream_t s) {
+    // four rows or more per request on average: prompts or chunks of them
+    if ((int64_t)a.T >= 4 * (int64_t)a.B) {
+        a.chunk = 32;
+        return launch_pdl(kv8_append_kernel<D, BF16, 4>, dim3((unsigned)((a.T + 31) / 32), (unsigned)a.Hkv, 2), dim3(KW_WARPS * 32), 0, s, a);
+    }
+    // a decode step's rows are a unit each: a CTA each while there are few
+    const int pairs = (a.Hkv + 1) / 2;
+    a.chunk = 1;
+    while (a.chunk < 32 && (int64_t)((a.T + a.chunk - 1) / a.chunk) * pairs > 4 * sm_count()) a.chunk *= 2;
+    return launch_pdl(kv8_append_kernel<D, BF16, 1>, dim3((unsigned)((a.T + a.chunk - 1) / a.chunk), (unsigned)pairs), dim3(KW_WARPS * 32), 0, s, a);
 }
 
 cudaError_t launch_kv8_append(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, const void* k, const void* v, int64_t x_row, int T, aq_dtype_t dt,
@@ -304,16 +365,11 @@ cudaError_t launch_kv8_append(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, 
     a.B = b.n_seqs; a.T = T; a.n_each = T / b.n_seqs; a.Hkv = c.n_kv_heads;
     a.shift = 0;
     while ((AQ_KV8_BLOCK << a.shift) < c.page) ++a.shift;
-    // rows per CTA: a decode step's rows are a unit each and get a CTA each; of a prompt's rows one in 32 leads a unit
-    const int pairs = (c.n_kv_heads + 1) / 2;
-    a.chunk = 1;
-    while (a.chunk < 32 && (int64_t)((T + a.chunk - 1) / a.chunk) * pairs > 4 * sm_count()) a.chunk *= 2;
-    const dim3 grid((unsigned)((T + a.chunk - 1) / a.chunk), (unsigned)pairs), block(KW_WARPS * 32);
-    cudaError_t e;
     const bool bf = dt == AQ_BF16;
-    if (c.head_dim == 64) e = bf ? launch_pdl(kv8_append_kernel<64, true>, grid, block, 0, s, a) : launch_pdl(kv8_append_kernel<64, false>, grid, block, 0, s, a);
-    else if (c.head_dim == 128) e = bf ? launch_pdl(kv8_append_kernel<128, true>, grid, block, 0, s, a) : launch_pdl(kv8_append_kernel<128, false>, grid, block, 0, s, a);
-    else e = bf ? launch_pdl(kv8_append_kernel<256, true>, grid, block, 0, s, a) : launch_pdl(kv8_append_kernel<256, false>, grid, block, 0, s, a);
+    cudaError_t e;
+    if (c.head_dim == 64) e = bf ? launch_kw<64, true>(a, s) : launch_kw<64, false>(a, s);
+    else if (c.head_dim == 128) e = bf ? launch_kw<128, true>(a, s) : launch_kw<128, false>(a, s);
+    else e = bf ? launch_kw<256, true>(a, s) : launch_kw<256, false>(a, s);
     count_launch();
     return e;
 }

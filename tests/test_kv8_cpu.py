@@ -119,6 +119,7 @@ def test_rope_refuses(aq):
                dict(dt=3), dict(odt=3), dict(T=0), dict(H=0), dict(D=32), dict(xs=1023), dict(os_=1000), dict(T=1 << 28), dict(rope=aq.Rope()),
                dict(o=FAKE, os_=2048), dict(dt=2, odt=0, o=FAKE)):
         assert rows(**kw) == aq.AQ_ERR_INVALID_ARG, kw
+    assert rows(D=1026, xs=1 << 20, os_=1 << 20) == aq.AQ_ERR_UNSUPPORTED and rows(H=4097, xs=1 << 20, os_=1 << 20) == aq.AQ_ERR_UNSUPPORTED
     assert rows(dt=0, odt=1) == aq.AQ_ERR_UNSUPPORTED and rows(dt=0, odt=2) == aq.AQ_ERR_UNSUPPORTED
 
 
