@@ -29,22 +29,24 @@ namespace aq {
 constexpr int KA_TILE = AQ_KV8_BLOCK;                 // positions per tile: the span of a scale
 constexpr int KA_MAX_CTAS = 192;
 
-// QT: groups of four query rows.  A warp's ring holds TILES tiles, keys and values copied and waited for separately, each refilled when it has
-// been used.  The first of a run's items may leave a piece, which takes the place of a tile: the ring is one shorter from then on.
+// QT: groups of four query rows.  A warp's ring has HALVES places; a place holds a tile's keys or its values, copied and waited for on their
+// own, and is filled again with what comes HALVES later when it has been used.  The first of a run's items may leave a piece: it takes
+// STEAL places, and the ring is that much shorter from then on.
 template <int D, int QT>
 struct KaShape {
-    static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : D == 128 ? 8 : 6;
-    static constexpr int TILES = D == 256 ? 2 : 3;
+    static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : 8;
+    static constexpr int HALVES = D == 256 ? 3 : 6;
     static constexpr int ROWS = 4 * QT;               // query rows of an item
     static constexpr int HALF = KA_TILE * D;          // bytes of a tile's keys (or values)
-    static constexpr int BUF = HALF + 16;             // + their scale and, with the keys, whether the tile may be read
     static constexpr int PITCH = D + 4;               // floats: a row's O, then its maximum and sum
     static constexpr int SLOT = ROWS * PITCH * 4;     // a piece
-    static constexpr int PLACE = 2 * BUF > SLOT ? 2 * BUF : SLOT;
-    static constexpr int RING = WARPS * TILES * PLACE;
+    static constexpr int STEAL = QT <= 2 ? 1 : 2;
+    static constexpr int BUF = HALF + 16;             // a half, its scale and, with keys, whether the tile may be read
+    static constexpr int PLACE = BUF > SLOT / STEAL ? BUF : SLOT / STEAL;
+    static constexpr int RING = WARPS * HALVES * PLACE;
     static constexpr int SMEM = RING + ROWS * 32 * 12;   // + for merging: a weight, a maximum and a sum per row and part
     static_assert((AQ_KV8_MAX_SEQS + 1) * 4 <= RING && 14 * SLOT <= RING, "the line's marks, and the parts of a group, lie in the ring");
-    static_assert(TILES >= 2 && 2 * WARPS <= 32, "a tile's place can be spared; a lane per piece");
+    static_assert(HALVES - STEAL >= 2 && (STEAL == 1 || HALVES % 2 == 0) && 2 * WARPS <= 32, "places can be spared; a lane per piece");
     static_assert(SMEM + 1300 <= 232448 && PLACE % 16 == 0, "shared memory of an SM");
 };
 // scratch: tickets [2][KA_MAX_CTAS], parts [KA_MAX_CTAS][4][rows][pitch]
@@ -275,10 +277,10 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         else j = (int)(off - KV8_ITEM_COST);
     }
 
-    const uint32_t my_ring = (uint32_t)(warp * S::TILES * S::PLACE), ring = (uint32_t)__cvta_generic_to_shared(smem) + my_ring;
+    const uint32_t my_ring = (uint32_t)(warp * S::HALVES * S::PLACE), ring = (uint32_t)__cvta_generic_to_shared(smem) + my_ring;
 
     if (x0 < x1) {
-        // ---- copies: a walk of its own, TILES tiles ahead ----------------------------------------------------
+        // ---- copies: a walk of its own, HALVES halves ahead --------------------------------------------------
         KaSeq ps = sq;
         int p_item = item, p_j = j, p_page0 = -1, p_pages = -1;   // lane i holds the number of page p_page0 + i
         uint32_t p_x = x0;
@@ -333,45 +335,43 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 ka_cp16(dst + ka_at<D>(lane / (D / 16) + i % REP * RPP, lane % (D / 16)) + i / REP * (REP * 512), src + i * 512);
             if (lane == 0) ka_cp4(dst + S::HALF, scales + p_blk);
         };
-        auto issue_keys = [&](int st) {
+        bool p_values = false;   // what is due: a tile's keys, or the values of the tile whose keys came last
+        auto issue = [&](int st) {
             const uint32_t dst = ring + (uint32_t)(st * S::PLACE);
-            const int pg = p_j >> a.shift;
-            if (p_page0 < 0 || pg >= p_page0 + 32 || pg < p_page0) {
-                p_page0 = pg;
-                const int i = pg + lane;
-                p_pages = (int64_t)i < a.width && (i << (a.shift + 5)) < ps.L ? __ldg(a.table + (int64_t)ps.b * a.width + i) : -1;
-            }
-            const int page = __shfl_sync(0xffffffffu, p_pages, pg - p_page0);
-            p_ok = page >= 0 && page < a.n_pages;
-            if (p_ok) {
+            if (!p_values) {
+                if (p_x >= x1) return;
+                const int pg = p_j >> a.shift;
+                if (p_page0 < 0 || pg >= p_page0 + 32 || pg < p_page0) {
+                    p_page0 = pg;
+                    const int i = pg + lane;
+                    p_pages = (int64_t)i < a.width && (i << (a.shift + 5)) < ps.L ? __ldg(a.table + (int64_t)ps.b * a.width + i) : -1;
+                }
+                const int page = __shfl_sync(0xffffffffu, p_pages, pg - p_page0);
+                p_ok = page >= 0 && page < a.n_pages;
                 const int hk = ps.rb == 1 ? p_item : p_item / ps.rb;
                 p_blk = (((int64_t)page * a.Hkv + hk) << a.shift) + (p_j & ((1 << a.shift) - 1));
-                copy(dst, a.kc, a.ks);
-            } else if (ps.L > 0 && lane == 0) {
-                kv8_report(KV8_BAD_PAGE);
+                if (!p_ok && ps.L > 0 && lane == 0) kv8_report(KV8_BAD_PAGE);
+                if (lane == 1) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + S::HALF + 4), "r"(p_ok ? 1 : 0) : "memory");
             }
-            if (lane == 1) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + S::HALF + 4), "r"(p_ok ? 1 : 0) : "memory");
-        };
-        auto issue_values = [&](int st) {   // of the tile whose keys were issued last; then on to the next
-            if (p_ok) copy(ring + (uint32_t)(st * S::PLACE + S::BUF), a.vc, a.vs);
-            ++p_x;
-            if (++p_j == ps.nt) {
-                p_x += KV8_ITEM_COST;
-                if (p_x < x1) {
-                    p_j = 0;
-                    const int was = ps.b;
-                    next_item(ps, p_item);
-                    if (ps.b != was) p_page0 = -1;
-                    touch_queries(ps, p_item);
+            if (p_ok) copy(dst, p_values ? a.vc : a.kc, p_values ? a.vs : a.ks);
+            if (p_values) {
+                ++p_x;
+                if (++p_j == ps.nt) {
+                    p_x += KV8_ITEM_COST;
+                    if (p_x < x1) {
+                        p_j = 0;
+                        const int was = ps.b;
+                        next_item(ps, p_item);
+                        if (ps.b != was) p_page0 = -1;
+                        touch_queries(ps, p_item);
+                    }
                 }
             }
+            p_values = !p_values;
         };
 #pragma unroll 1
-        for (int s = 0; s < S::TILES; ++s) {
-            const bool more = p_x < x1;
-            if (more) issue_keys(s);
-            ka_commit();
-            if (more) issue_values(s);
+        for (int s = 0; s < S::HALVES; ++s) {
+            issue(s);
             ka_commit();
         }
 
@@ -381,7 +381,12 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         int lim[QT], lim_min = 0;
         KaPiece pc{};
         bool fresh = true;
-        int st = 0, gone = -1;        // the tile's place; the place that a piece has taken
+        int kst = 0, gone = -1;       // the place of the tile's keys; the first one that a piece has taken
+        auto after = [&](int st) {
+            st = st + 1 == S::HALVES ? 0 : st + 1;
+            if (st == gone) st = st + S::STEAL >= S::HALVES ? st + S::STEAL - S::HALVES : st + S::STEAL;
+            return st;
+        };
         for (uint32_t x = x0; x < x1;) {
             if (fresh) {   // ---- another item: its queries
                 fresh = false;
@@ -451,9 +456,10 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             const bool item_ends = j + 1 == sq.nt;
             const uint32_t next = x + 1 + (item_ends ? KV8_ITEM_COST : 0u);
             const bool run_ends = next >= x1, whole = item_ends && pc.first >= x0, take = item_ends && !run_ends && !whole;
-            if (gone < 0) ka_wait<2 * S::TILES - 1>(); else ka_wait<2 * S::TILES - 3>();
+            if (gone < 0) ka_wait<S::HALVES - 1>(); else ka_wait<S::HALVES - 1 - S::STEAL>();
             __syncwarp();   // every lane's copies of the keys have landed
-            const uint32_t kt = ring + (uint32_t)(st * S::PLACE), vt = kt + S::BUF;
+            const int vst = after(kst);
+            const uint32_t kt = ring + (uint32_t)(kst * S::PLACE), vt = ring + (uint32_t)(vst * S::PLACE);
             float ks;
             int ok;
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(kt + S::HALF) : "memory");
@@ -478,12 +484,12 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 }
             }
             __syncwarp();   // every lane is through with the keys
-            const bool more = p_x < x1 && !take;
-            if (more) issue_keys(st);
-            if (take) ka_wait<2 * S::TILES - 2>();
-            else {
+            if (take && S::STEAL == 2) {
+                ka_wait<S::HALVES - 2>();
+            } else {
+                issue(kst);
                 ka_commit();
-                if (gone < 0) ka_wait<2 * S::TILES - 1>(); else ka_wait<2 * S::TILES - 3>();
+                if (gone < 0) ka_wait<S::HALVES - 1>(); else ka_wait<S::HALVES - 1 - S::STEAL>();
             }
             __syncwarp();   // every lane's copies of the values have landed
             if (ok) {
@@ -563,8 +569,10 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 }
             }
             __syncwarp();   // every lane is through with the values
-            if (more) issue_values(st);
-            if (!take) ka_commit();
+            if (!take) {
+                issue(vst);
+                ka_commit();
+            }
 
             // ---- the item's end, or the run's
             if (item_ends || run_ends) {
@@ -584,7 +592,8 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     }
                 } else {
                     // the run's first piece, where this tile was, or its last: all copies have been used by then
-                    pc.at = my_ring + (uint32_t)(st * S::PLACE);
+                    const int to = S::STEAL == 1 ? vst : kst;   // (places of one tile lie side by side where two are wanted)
+                    pc.at = my_ring + (uint32_t)(to * S::PLACE);
 #pragma unroll
                     for (int u = 0; u < QT; ++u) {
                         float* row = reinterpret_cast<float*>(smem + pc.at) + (4 * u + t) * S::PITCH;
@@ -593,11 +602,10 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                         if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(m[u], l[u]);
                     }
                     if (lane == 0) pieces[2 * warp + (run_ends ? 1 : 0)] = pc;
-                    if (take) gone = st;
+                    if (take) gone = to;
                 }
             }
-            st = st + 1 == S::TILES ? 0 : st + 1;
-            if (st == gone) st = st + 1 == S::TILES ? 0 : st + 1;
+            kst = after(vst);
             if (item_ends) {
                 j = 0;
                 if (!run_ends) { next_item(sq, item); fresh = true; }
@@ -617,7 +625,8 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     float (*weight)[32] = reinterpret_cast<float (*)[32]>(smem + S::RING + ROWS * 32 * 8);
     auto weigh = [&](unsigned there, unsigned heads, uint32_t my_at, int rows) {
         const unsigned upto = heads & ((2u << lane) - 1u), later = heads & ~((2u << lane) - 1u);
-        const int lo = upto ? 31 - __clz(upto) : 0, hi = later ? __ffs(later) - 2 : 31;
+        // (its last part's lane, not the lane before the next group: sums then go in an order of the group's own, whatever lies beside it)
+        const int lo = upto ? 31 - __clz(upto) : 0, hi = max(31 - __clz((int)(there & (later ? (later & (0u - later)) - 1u : 0xffffffffu))), 0);
         for (int r = warp; r < rows; r += W) {
             float2 ml = make_float2(-INFINITY, 0.f);
             if (there >> lane & 1u) ml = *reinterpret_cast<const float2*>(smem + my_at + (r * S::PITCH + D) * 4);
@@ -642,12 +651,19 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     };
     auto sum_parts = [&](unsigned there, int k0, int k1, int r, int d, auto at) -> float4 {   // parts k0 .. k1 - 1, those of `there`
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int k = k0; k < k1; ++k) {
-            if (!(there >> k & 1u)) continue;
-            const float4 y = *reinterpret_cast<const float4*>(smem + at(k) + (r * S::PITCH + d) * 4);
-            const float w = weight[r][k];
-            o.x = fmaf(w, y.x, o.x); o.y = fmaf(w, y.y, o.y); o.z = fmaf(w, y.z, o.z); o.w = fmaf(w, y.w, o.w);
+        for (int k = k0; k < k1; k += 4) {
+            float4 y[4];
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool in = k + i < k1 && (there >> (k + i) & 1u);
+                y[i] = in ? *reinterpret_cast<const float4*>(smem + at(k + i) + (r * S::PITCH + d) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                w[i] = in ? weight[r][k + i] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o.x = fmaf(w[i], y[i].x, o.x); o.y = fmaf(w[i], y[i].y, o.y); o.z = fmaf(w[i], y[i].z, o.z); o.w = fmaf(w[i], y[i].w, o.w);
+            }
         }
         return o;
     };
@@ -716,22 +732,19 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             last_flag[k] = last ? 1 : 0;
         }
         __syncthreads();
+        const int n0 = last_flag[0] ? entries[0] : 0, n1 = last_flag[1] ? entries[1] : 0;
         bool more = false;
-#pragma unroll 1
-        for (int k = 0; k < 2; ++k) {
-            const int n = k == 0 ? entries[0] : entries[1];
-            if (n == 0 || !last_flag[k]) {
-                if (k == 0) open0 = -1; else open1 = -1;
-                continue;
-            }
-            const KaPiece pc = pieces[k == 0 ? open0 : open1];
-            const int base = k == 0 ? f[0] : f[1], l = k == 0 ? lo[0] : lo[1], st = k == 0 ? step[0] : step[1];
-            const bool fin = k == 0 ? final[0] : final[1];
-            const int rows = min(ROWS, pc.rows - pc.q0), pieces16 = rows * S::PITCH / 4;   // 16-byte pieces of an entry
+        // both at once where there is room
+        for (int todo = (n0 ? 1 : 0) | (n1 ? 2 : 0); todo;) {
+            const int now = todo == 3 && (n0 + n1) * S::SLOT > S::RING ? 1 : todo;
+            todo &= ~now;
+            const int m0 = now & 1 ? n0 : 0, m = m0 + (now & 2 ? n1 : 0);   // entries 0 .. m0 - 1 of the one item, m0 .. m - 1 of the other
             const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem);
-            for (int e = warp; e < n; e += W) {
-                const int c = l + e * st;
-                const uint8_t* src = a.part + ((size_t)(base + c) * 4 + (level == 1 ? 2 : 0) + (c == 0 ? 1 : 0)) * S::SLOT;
+            auto rows_of = [&](int k) { const KaPiece& pc = pieces[k == 0 ? open0 : open1]; return min(ROWS, pc.rows - pc.q0); };
+            for (int e = warp; e < m; e += W) {
+                const int k = e < m0 ? 0 : 1, c = (k == 0 ? lo[0] : lo[1]) + (e - (k == 0 ? 0 : m0)) * (k == 0 ? step[0] : step[1]);
+                const uint8_t* src = a.part + ((size_t)((k == 0 ? f[0] : f[1]) + c) * 4 + (level == 1 ? 2 : 0) + (c == 0 ? 1 : 0)) * S::SLOT;
+                const int pieces16 = rows_of(k) * S::PITCH / 4;   // 16-byte pieces of an entry
 #pragma unroll 4
                 for (int i = lane; i < pieces16; i += 32) ka_cp16(dst + e * S::SLOT + i * 16, src + i * 16);
             }
@@ -739,17 +752,20 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             ka_wait<0>();
             __syncthreads();
             auto at = [](int e) -> uint32_t { return (uint32_t)(e * S::SLOT); };
-            const unsigned there = (1u << n) - 1u;
-            weigh(there, 1u, at(min(lane, n - 1)), rows);
+            const unsigned there = m == 32 ? 0xffffffffu : (1u << m) - 1u, heads = (m0 ? 1u : 0u) | (m > m0 ? 1u << m0 : 0u);
+            weigh(there, heads, at(min(lane, m - 1)), ROWS);   // (what it makes of rows that an item does not have is not used)
             __syncthreads();
-            for (int i = threadIdx.x; i < rows * (D / 4); i += W * 32) {
-                const int r = i / (D / 4), d = i % (D / 4) * 4;
-                put(pc, r, d, 0, sum_parts(there, 0, n, r, d, at), fin, (size_t)(base + l) * 4 + (l == 0 ? 3 : 2));
+            for (int i = threadIdx.x; i < __popc(heads) * ROWS * (D / 4); i += W * 32) {
+                const int k = (m0 == 0 || i >= ROWS * (D / 4)) ? 1 : 0, r = i / (D / 4) % ROWS, d = i % (D / 4) * 4;
+                if (r >= rows_of(k)) continue;
+                const KaPiece& pc = pieces[k == 0 ? open0 : open1];
+                put(pc, r, d, k == 0 ? 0 : m0, sum_parts(there, k == 0 ? 0 : m0, k == 0 ? m0 : m, r, d, at), k == 0 ? final[0] : final[1],
+                    (size_t)((k == 0 ? f[0] : f[1]) + (k == 0 ? lo[0] : lo[1])) * 4 + ((k == 0 ? lo[0] : lo[1]) == 0 ? 3 : 2));
             }
-            if (fin) { if (k == 0) open0 = -1; else open1 = -1; }
-            else more = true;
             __syncthreads();   // (the next merge uses the same shared memory)
         }
+        if (n0 && !final[0]) more = true; else open0 = -1;
+        if (n1 && !final[1]) more = true; else open1 = -1;
         if (!more) return;
     }
 }
