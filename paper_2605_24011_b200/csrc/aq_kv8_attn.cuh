@@ -34,8 +34,8 @@ constexpr int KA_MAX_CTAS = 192;
 // STEAL places, and the ring is that much shorter from then on.
 template <int D, int QT>
 struct KaShape {
-    static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : 8;
-    static constexpr int HALVES = D == 256 ? 3 : 6;
+    static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : D == 128 && QT <= 3 ? 12 : 8;
+    static constexpr int HALVES = D == 256 ? 3 : D == 128 && QT <= 3 ? 4 : 6;
     static constexpr int ROWS = 4 * QT;               // query rows of an item
     static constexpr int HALF = KA_TILE * D;          // bytes of a tile's keys (or values)
     static constexpr int PITCH = D + 4;               // floats: a row's O, then its maximum and sum
@@ -47,7 +47,7 @@ struct KaShape {
     static constexpr int SMEM = RING + ROWS * 32 * 12;   // + for merging: a weight, a maximum and a sum per row and part
     static_assert((AQ_KV8_MAX_SEQS + 1) * 4 <= RING && 14 * SLOT <= RING, "the line's marks, and the parts of a group, lie in the ring");
     static_assert(HALVES - STEAL >= 2 && (STEAL == 1 || HALVES % 2 == 0) && 2 * WARPS <= 32, "places can be spared; a lane per piece");
-    static_assert(SMEM + 1300 <= 232448 && PLACE % 16 == 0, "shared memory of an SM");
+    static_assert(SMEM + 2600 <= 232448 && PLACE % 16 == 0, "shared memory of an SM");
 };
 // scratch: tickets [2][KA_MAX_CTAS], parts [KA_MAX_CTAS][4][rows][pitch]
 constexpr size_t KA_TICKET_BYTES = 2 * KA_MAX_CTAS * 4;
@@ -181,6 +181,8 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     __shared__ KaPiece pieces[2 * W];
     __shared__ uint32_t sums[W][2];
     __shared__ int last_flag[2], group_head[32];
+    __shared__ KaSeq seqs[2 * W];   // the requests that a warp's copies and its products are at (kept out of the registers)
+    __shared__ KaPiece at_work[W];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, t = lane & 3;
 
@@ -281,14 +283,23 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
 
     if (x0 < x1) {
         // ---- copies: a walk of its own, HALVES halves ahead --------------------------------------------------
-        KaSeq ps = sq;
+        KaSeq& ps = seqs[2 * warp];
+        KaSeq& cs = seqs[2 * warp + 1];
+        if (lane == 0) ps = cs = sq;
+        __syncwarp();
         int p_item = item, p_j = j, p_page0 = -1, p_pages = -1;   // lane i holds the number of page p_page0 + i
+        int nt = sq.nt;
         uint32_t p_x = x0;
-        auto next_item = [&](KaSeq& s, int& it) {
-            if (++it < s.rb * a.Hkv) return;
+        auto next_item = [&](KaSeq& s, int& it) {   // whether the request is another one now
+            if (++it < s.rb * a.Hkv) return false;
             it = 0;
             int b = s.b;
-            do { s = ka_seq(a, ++b, ROWS); } while (s.n == 0 && b + 1 < a.B);   // (x < total: there is one)
+            KaSeq to;
+            do { to = ka_seq(a, ++b, ROWS); } while (to.n == 0 && b + 1 < a.B);   // (x < total: there is one)
+            __syncwarp();
+            if (lane == 0) s = to;
+            __syncwarp();
+            return true;
         };
         auto touch_queries = [&](const KaSeq& s, int it) {   // a line per lane, so that they are near when the item's turn comes
             constexpr int LINES = D * 2 / 128;
@@ -301,7 +312,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         };
         // an item's query rows as they come: of row 4 u + g / 2, dims 32 c + 4 t .. and 16 further.  The first item's are asked for before its
         // tiles where there are registers for that.
-        constexpr bool EARLY = QT * D <= 256;
+        constexpr bool EARLY = QT <= 2;
         uint2 raw[EARLY ? QT : 1][D / 32][2];
         auto load_queries = [&](const KaSeq& s, int it, int u0) {
             const int hk = s.rb == 1 ? it : it / s.rb, q0 = (it - hk * s.rb) * ROWS;
@@ -323,7 +334,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 }
             }
         };
-        if constexpr (EARLY) load_queries(sq, item, 0);       // (under way while the first tiles' pages are looked up)
+        if constexpr (EARLY) load_queries(cs, item, 0);       // (under way while the first tiles' pages are looked up)
         bool p_ok = false;
         int64_t p_blk = 0;
         auto copy = [&](uint32_t dst, const uint8_t* codes, const float* scales) {   // a tile's keys or values, and their scale
@@ -360,9 +371,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     p_x += KV8_ITEM_COST;
                     if (p_x < x1) {
                         p_j = 0;
-                        const int was = ps.b;
-                        next_item(ps, p_item);
-                        if (ps.b != was) p_page0 = -1;
+                        if (next_item(ps, p_item)) p_page0 = -1;
                         touch_queries(ps, p_item);
                     }
                 }
@@ -379,7 +388,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         float o[QT][D / 16][2];       // of query row 4 u + t: dims 16 c + 2 g and the next
         float m[QT], l[QT], fq[QT];
         int lim[QT], lim_min = 0;
-        KaPiece pc{};
+        uint32_t first = 0;           // the place of the item's first tile
         bool fresh = true;
         int kst = 0, gone = -1;       // the place of the tile's keys; the first one that a piece has taken
         auto after = [&](int st) {
@@ -390,17 +399,22 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         for (uint32_t x = x0; x < x1;) {
             if (fresh) {   // ---- another item: its queries
                 fresh = false;
-                pc.first = x - (uint32_t)j;
-                pc.nt = sq.nt;
+                __syncwarp();   // (every lane has read the piece before)
+                const KaSeq sq = cs;
+                KaPiece pc;
+                pc.first = first = x - (uint32_t)j;
+                pc.nt = nt = sq.nt;
                 pc.row0 = sq.row0;
                 pc.rows = a.G * sq.n;
                 pc.hk = sq.rb == 1 ? item : item / sq.rb;
                 pc.q0 = (item - pc.hk * sq.rb) * ROWS;
+                pc.at = 0;
+                if (lane == 0) at_work[warp] = pc;
                 // operand column g of a group of four rows: row g / 2, plane g % 2
-                if constexpr (EARLY) { if (x != x0) load_queries(sq, item, 0); }
+                if constexpr (EARLY) { if (x != x0) load_queries(cs, item, 0); }
 #pragma unroll
                 for (int u = 0; u < QT; ++u) {
-                    if constexpr (!EARLY) load_queries(sq, item, u);
+                    if constexpr (!EARLY) load_queries(cs, item, u);
                     constexpr int U = EARLY ? 1 : 0;   // (whether raw holds all groups)
                     // magnitudes as whole numbers: of two values of one type the larger has the larger pattern, a NaN the largest
                     uint32_t most = 0;
@@ -453,9 +467,9 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 lim_min = sq.L - sq.n + (int)kv8_div((uint32_t)pc.q0, a.G_magic) + 1;
             }
 
-            const bool item_ends = j + 1 == sq.nt;
+            const bool item_ends = j + 1 == nt;
             const uint32_t next = x + 1 + (item_ends ? KV8_ITEM_COST : 0u);
-            const bool run_ends = next >= x1, whole = item_ends && pc.first >= x0, take = item_ends && !run_ends && !whole;
+            const bool run_ends = next >= x1, whole = item_ends && first >= x0, take = item_ends && !run_ends && !whole;
             if (gone < 0) ka_wait<S::HALVES - 1>(); else ka_wait<S::HALVES - 1 - S::STEAL>();
             __syncwarp();   // every lane's copies of the keys have landed
             const int vst = after(kst);
@@ -576,6 +590,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
 
             // ---- the item's end, or the run's
             if (item_ends || run_ends) {
+                KaPiece pc = at_work[warp];
                 if (whole) {
 #pragma unroll
                     for (int u = 0; u < QT; ++u) {
@@ -608,7 +623,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             kst = after(vst);
             if (item_ends) {
                 j = 0;
-                if (!run_ends) { next_item(sq, item); fresh = true; }
+                if (!run_ends) { next_item(cs, item); fresh = true; }
             } else {
                 ++j;
             }

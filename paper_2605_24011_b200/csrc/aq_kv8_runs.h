@@ -15,7 +15,7 @@
 
 namespace aq {
 
-constexpr uint32_t KV8_ITEM_COST = 1;
+constexpr uint32_t KV8_ITEM_COST = 2;
 
 // CTAs of a launch over a line of `total` places with `items` items, `warps` warps each, at most `most`.  Where there is a CTA for
 // every item and its warps have few tiles of it (five places), one each: nothing is then merged between CTAs, which costs a chain
