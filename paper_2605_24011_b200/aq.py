@@ -60,6 +60,7 @@ class _Kv8BatchC(C.Structure):
 
 class Rope(C.Structure):
     """aq_rope_t: the frequencies of a rotary embedding (aq_rope_setup)."""
+    addr = property(C.addressof)
     _fields_ = [("turns", C.c_double * 128), ("magnitude", C.c_float), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("pad_", C.c_int32)]
 
 
@@ -273,37 +274,40 @@ def aq_attn_decode(q, k_cache, v_cache, L: int, out, scratch, scale: float = 0.0
 
 # ---- a batch of requests over a paged cache held in 8 bits -----------------------------------------------------
 
-def _current_device() -> int:
-    """Index of torch's current device (first call: finds the cheapest way to ask and takes this function's place)."""
-    import torch
-    global _current_device
-    torch.cuda.current_device()
-    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    return _current_device()
-
-
-_INT = {}   # type code by torch's type, for the arrays that are not activations
+_TYPES = {}   # short names of torch's types, for the arrays that are not activations
 
 
 def _array(t, code, what):
     """Address of an array of a step or a cache; refuses what the library would read wrongly."""
-    if not _INT:
+    if not _TYPES:
         import torch
-        _INT.update({torch.int8: "i8", torch.int32: "i32", torch.float32: "f32"})
-    if _INT.get(t.dtype) != code or not t.is_contiguous() or t.get_device() < 0:
+        _TYPES.update({torch.int8: "i8", torch.int32: "i32", torch.float32: "f32"})
+    if _TYPES.get(t.dtype) != code or not t.is_contiguous() or t.get_device() < 0:
         raise ValueError(f"{what}: a contiguous CUDA tensor of type {code} is wanted, got {t.dtype} on {t.device}, strides {tuple(t.stride())}")
     return t.data_ptr()
 
 
-def _rows(t, what):
-    """Address and row stride of a step's rows [n_rows][heads][head_dim]: rows may be apart, a row's heads lie together."""
-    T, H, D = t.shape
-    stride, per_head, one = t.stride()
-    if (one != 1 and D > 1) or (per_head != D and H > 1):
-        raise ValueError(f"{what}: the heads of a row have to lie together, got strides {(stride, per_head, one)} for shape {(T, H, D)}")
-    if t.get_device() != _current_device():
-        raise ValueError(f"{what}: on {t.device}, and the current device is cuda:{_current_device()}")
-    return t.data_ptr(), (stride if T > 1 else H * D)
+class _Calls:
+    """The compiled calls (csrc/aq_torch.cpp), loaded and given the library's entry points when the first one is made."""
+
+    def __getattr__(self, name):
+        import importlib.machinery
+        import importlib.util
+
+        import torch  # noqa: F401  (the module needs its libraries loaded)
+        path = os.path.join(_HERE, "_aq_torch.so")
+        if not os.path.exists(path):
+            raise ImportError(f"{path} not found: build it with `python -m paper_2605_24011_b200.build`")
+        spec = importlib.util.spec_from_file_location("_aq_torch", path, loader=importlib.machinery.ExtensionFileLoader("_aq_torch", path))
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+        mod.bind(*(C.cast(f, C.c_void_p).value for f in (_lib.aq_kv8_plan, _lib.aq_kv8_append, _lib.aq_kv8_attn, _lib.aq_rope_rows)))
+        global _calls
+        _calls = mod
+        return getattr(mod, name)
+
+
+_calls = _Calls()
 
 
 class Kv8Cache:
@@ -344,36 +348,19 @@ class Kv8Batch:
         self.addr = C.addressof(self.c)
 
 
-def _kv8_device(cache, batch, where):
-    dev = _current_device()
-    if cache.device != dev or batch.device != dev:
-        raise ValueError(f"{where}: cache on cuda:{cache.device}, step on cuda:{batch.device}, and the current device is cuda:{dev}")
-
-
 def aq_kv8_plan(lens, new, table, free, n_free, page: int, lens_out, n_free_out, row_start, pos, stream=None):
     """All CUDA int32: lens, new, lens_out [n_seqs]; table [n_seqs][width]; free [capacity]; n_free, n_free_out [1]; row_start
     [n_seqs + 1]; pos [n_rows]."""
-    n, width = table.shape
-    if not (lens.numel() == new.numel() == lens_out.numel() == n and row_start.numel() == n + 1 and n_free.numel() == n_free_out.numel() == 1):
-        raise ValueError("aq_kv8_plan: lens, new, lens_out [n], table [n][width], row_start [n + 1], n_free, n_free_out [1] are wanted")
-    dev = _current_device()
-    p = []
-    for t, what in ((lens, "lens"), (new, "new"), (table, "table"), (free, "free"), (n_free, "n_free"), (lens_out, "lens_out"),
-                    (n_free_out, "n_free_out"), (row_start, "row_start"), (pos, "pos")):
-        p.append(_array(t, "i32", what))
-        if t.get_device() != dev:
-            raise ValueError(f"aq_kv8_plan: {what} on {t.device}, and the current device is cuda:{dev}")
-    _check(_lib.aq_kv8_plan(p[0], p[1], n, int(page), p[2], width, p[3], free.numel(), p[4], p[5], p[6], p[7], p[8], pos.numel(),
-                            _stream(stream)), "aq_kv8_plan")
+    st = _calls.plan(lens, new, table, free, n_free, page, lens_out, n_free_out, row_start, pos, None if stream is None else _stream(stream))
+    if st:
+        raise AqError(st, "aq_kv8_plan")
 
 
 def aq_kv8_append(cache: Kv8Cache, batch: Kv8Batch, k, v, stream=None):
     """k, v: CUDA float16 / bfloat16 [n_rows][n_kv_heads][head_dim], rows of one stride."""
-    _kv8_device(cache, batch, "aq_kv8_append")
-    (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
-    if k.shape != v.shape or ks != vs or k.dtype != v.dtype or k.shape[1] != cache.c.n_kv_heads or k.shape[2] != cache.c.head_dim:
-        raise ValueError(f"aq_kv8_append: k and v are rows of {cache.c.n_kv_heads} heads of {cache.c.head_dim} alike, got {tuple(k.shape)} and {tuple(v.shape)}")
-    _check(_lib.aq_kv8_append(cache.addr, batch.addr, kp, vp, ks, k.shape[0], dtype_code(k), _stream(stream)), "aq_kv8_append")
+    st = _calls.append(cache.addr, cache.device, batch.addr, batch.device, k, v, None if stream is None else _stream(stream))
+    if st:
+        raise AqError(st, "aq_kv8_append")
 
 
 def aq_kv8_scratch(device=None):
@@ -385,12 +372,9 @@ def aq_kv8_scratch(device=None):
 def aq_kv8_attn(cache: Kv8Cache, batch: Kv8Batch, q, out, scratch, scale: float = 0.0, stream=None):
     """q: CUDA float16 / bfloat16 [n_rows][n_heads][head_dim]; out: CUDA, the shape of q, any of the three types; scratch: CUDA uint8 of
     AQ_KV8_SCRATCH_BYTES, zeroed before its first use (aq_kv8_scratch); calls that may overlap need scratch of their own."""
-    _kv8_device(cache, batch, "aq_kv8_attn")
-    (qp, qs), (op, os_) = _rows(q, "q"), _rows(out, "out")
-    if q.shape != out.shape or q.shape[2] != cache.c.head_dim or scratch.get_device() != cache.device:
-        raise ValueError(f"aq_kv8_attn: q and out are rows of heads of {cache.c.head_dim} alike, scratch on their device, got {tuple(q.shape)} and {tuple(out.shape)}")
-    _check(_lib.aq_kv8_attn(cache.addr, batch.addr, qp, qs, op, os_, q.shape[0], q.shape[1], float(scale), dtype_code(q), dtype_code(out),
-                            scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)), "aq_kv8_attn")
+    st = _calls.attn(cache.addr, cache.device, batch.addr, batch.device, q, out, scratch, scale, None if stream is None else _stream(stream))
+    if st:
+        raise AqError(st, "aq_kv8_attn")
     return out
 
 
@@ -407,12 +391,9 @@ def aq_rope_rows(rope: Rope, x, pos, out=None, stream=None):
     """x: CUDA [n_rows][n_heads][head_dim], any of the three types; pos: CUDA int32 [n_rows] (negative: the row is left as it is); out: like
     x, of its type or, for float32, a half type; None: in place."""
     out = x if out is None else out
-    (xp, xs), (op, os_) = _rows(x, "x"), _rows(out, "out")
-    T, H, D = x.shape
-    if out.shape != x.shape or pos.numel() != T or pos.get_device() != x.get_device():
-        raise ValueError(f"aq_rope_rows: out like x and a position per row are wanted, got {tuple(x.shape)}, {tuple(out.shape)}, {tuple(pos.shape)}")
-    _check(_lib.aq_rope_rows(C.byref(rope), xp, dtype_code(x), xs, op, dtype_code(out), os_, T, H, D, _array(pos, "i32", "pos"),
-                             _stream(stream)), "aq_rope_rows")
+    st = _calls.rope(rope.addr, x, pos, out, None if stream is None else _stream(stream))
+    if st:
+        raise AqError(st, "aq_rope_rows")
     return out
 
 

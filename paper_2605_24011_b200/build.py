@@ -1,4 +1,4 @@
-"""Builds libaq.so (CUDA, sm_100a only) next to this file with nvcc.
+"""Builds libaq.so (CUDA, sm_100a only) next to this file with nvcc, and _aq_torch.so (its calls on torch tensors) with the host compiler.
 
     python -m paper_2605_24011_b200.build [--force]
 
@@ -14,6 +14,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libaq.so")
+TORCH_OUT = os.path.join(HERE, "_aq_torch.so")
 OBJ = os.path.join(HERE, "_build")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -40,13 +41,35 @@ def _compile(src):
     return obj
 
 
+def _compile_torch():
+    """_aq_torch.so, against the torch that this interpreter has (its headers and libraries, no others)."""
+    src = os.path.join(CSRC, "aq_torch.cpp")
+    deps = max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "aq.h")))
+    if os.path.exists(TORCH_OUT) and os.path.getmtime(TORCH_OUT) >= deps:
+        return
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+           os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")]
+    lib = os.path.join(root, "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{i}" for i in inc), src,
+           "-o", TORCH_OUT, f"-L{lib}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on aq_torch.cpp:\n{r.stdout}\n{r.stderr}")
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ for sm_100a and link libaq.so."""
-    if not force and os.path.exists(OUT) and os.path.getmtime(OUT) >= _deps_mtime():
+    """Compile every .cu under csrc/ for sm_100a and link libaq.so; compile aq_torch.cpp."""
+    if not force and os.path.exists(OUT) and os.path.getmtime(OUT) >= _deps_mtime() and os.path.exists(TORCH_OUT):
         return OUT
     os.makedirs(OBJ, exist_ok=True)
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
+        binding = ex.submit(_compile_torch)
         objs = list(ex.map(_compile, _sources()))
+        binding.result()
     cmd = [NVCC, "-shared", "-o", OUT, *objs, "-cudart", "static"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

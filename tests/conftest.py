@@ -16,9 +16,9 @@ def pytest_configure(config):
 
 @pytest.fixture(scope="session", autouse=True)
 def _built_library():
-    """Build libaq.so when it is missing and nvcc is present (no GPU needed)."""
+    """Build what is missing of libaq.so and its calls on torch tensors when nvcc is present (no GPU needed)."""
     from paper_2605_24011_b200 import build as B
-    if not os.path.exists(B.OUT) and os.path.exists(B.NVCC):
+    if not (os.path.exists(B.OUT) and os.path.exists(B.TORCH_OUT)) and os.path.exists(B.NVCC):
         B.build()
     yield
 

@@ -137,8 +137,14 @@ def test_binding_refuses_tensors_that_the_library_would_misread(aq):
         aq.Kv8Batch(torch.zeros(3, dtype=torch.int32), torch.zeros(4, 2, dtype=torch.int32))
     with pytest.raises(ValueError):
         aq.Kv8Batch(torch.zeros(4, dtype=torch.int32), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, dtype=torch.int32))
-    with pytest.raises(ValueError):
-        aq._rows(torch.zeros(4, 8, 3)[:, ::2], "q")   # a row's heads apart
+    i = torch.zeros(4, dtype=torch.int32)
+    x = torch.zeros(4, 8, 64)
+    class D:                                       # a descriptor's place
+        addr, device = FAKE, 0
+    for call in (lambda: aq.aq_kv8_plan(i, i, i.view(2, 2), i, i, 64, i, i, i, i), lambda: aq.aq_rope_rows(aq.aq_rope_setup(64), x, i),
+                 lambda: aq.aq_kv8_append(D, D, x, x), lambda: aq.aq_kv8_attn(D, D, x, x, i)):
+        with pytest.raises((ValueError, RuntimeError)):   # (RuntimeError: no device at all)
+            call()
 
 
 # ---- the line of tiles -------------------------------------------------------------------------------------------
