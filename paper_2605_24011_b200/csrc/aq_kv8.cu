@@ -177,9 +177,9 @@ struct KwArgs {
     const int32_t* row_start;
     const int32_t* table;
     int64_t width, n_pages, x_row;
-    int B, T, n_each, Hkv, shift, chunk;   // shift: log2(blocks per page); chunk: rows per CTA
+    int B, T, n_each, Hkv, shift, chunk, heads;   // shift: log2(blocks per page); rows per CTA; heads per CTA (WPU 4)
 };
-constexpr int KW_WARPS = 4;
+constexpr int KW_WARPS = 4, KW_CTAS = 6;
 
 __device__ __forceinline__ float kw_up11(float x) { return __uint_as_float((__float_as_uint(x) + 0x1FFFu) & ~0x1FFFu); }
 
@@ -193,20 +193,38 @@ __device__ __forceinline__ uint32_t kw_bytes(uint32_t a, uint32_t b, uint32_t c,
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 
-// WPU warps of a unit (1, or the CTA's 4, all of which call this together): w is this one's number among them.
-template <int D, bool BF16, int WPU>
-__device__ __forceinline__ void kw_unit(const uint16_t* x, int64_t x_row, int n, int at, uint8_t* codes, float* scale, int w, uint32_t* meet) {
-    constexpr int LPR = D / 8;                // lanes per row (16 bytes each)
-    constexpr int RPP = 32 / LPR * WPU;       // rows per pass
-    constexpr int NV = 32 / RPP;              // passes of a whole block
-    const int lane = threadIdx.x & 31, sub = w * (32 / LPR) + lane / LPR, c = lane % LPR;
+// A unit's rows on their way, in the registers of its WPU warps (1, or the CTA's 4): w is this one's number among them.
+template <int D, int WPU>
+struct KwUnit {
+    static constexpr int LPR = D / 8;                // lanes per row (16 bytes each)
+    static constexpr int RPP = 32 / LPR * WPU;       // rows per pass
+    static constexpr int NV = 32 / RPP;              // passes of a whole block
     uint4 v[NV];
+    float s_old;
+    int n, at;
+    uint8_t* codes;
+    float* scale;
+    __device__ __forceinline__ void load(const uint16_t* x, int64_t x_row, int n_, int at_, uint8_t* codes_, float* scale_, int w) {
+        const int lane = threadIdx.x & 31, sub = w * (32 / LPR) + lane / LPR, c = lane % LPR;
+        n = n_; at = at_; codes = codes_; scale = scale_;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int r = i * RPP + sub;
-        v[i] = r < n ? __ldg(reinterpret_cast<const uint4*>(x + r * x_row) + c) : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < NV; ++i) {
+            const int r = i * RPP + sub;
+            v[i] = r < n ? __ldg(reinterpret_cast<const uint4*>(x + r * x_row) + c) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        s_old = at > 0 ? *scale : 0.f;
     }
-    const float s_old = at > 0 ? *scale : 0.f;
+};
+
+// Quantises and stores a unit; all of its warps call this together.
+template <int D, bool BF16, int WPU>
+__device__ __forceinline__ void kw_store(const KwUnit<D, WPU>& u, int w, uint32_t* meet) {
+    constexpr int LPR = KwUnit<D, WPU>::LPR, RPP = KwUnit<D, WPU>::RPP, NV = KwUnit<D, WPU>::NV;
+    const int lane = threadIdx.x & 31, sub = w * (32 / LPR) + lane / LPR, c = lane % LPR, n = u.n, at = u.at;
+    const uint4 (&v)[NV] = u.v;
+    const float s_old = u.s_old;
+    uint8_t* codes = u.codes;
+    float* scale = u.scale;
     // magnitudes as whole numbers: of two values of one 16-bit type the larger has the larger pattern, a NaN the largest
     uint32_t most = 0;
 #pragma unroll
@@ -283,14 +301,14 @@ __device__ __forceinline__ void kw_unit(const uint16_t* x, int64_t x_row, int n,
 }
 
 // WPU 1: a warp per unit, two heads' keys and values per CTA (decode steps: units of a row or a few).  WPU 4: the CTA's warps share each
-// unit, a head's keys or values per CTA (prompts: one warp per unit left an SM with a few thousand instructions in a row, 9 requests'
+// unit, keys or values of a few heads per CTA (prompts: one warp per unit left an SM with a few thousand instructions in a row, 9 requests'
 // chunks of 333 rows of one head of 256 took 14.0 us).
 template <int D, bool BF16, int WPU>
 __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_constant__ KwArgs a) {
     __shared__ int begin[AQ_KV8_MAX_SEQS + 1];
     __shared__ uint32_t meet[KW_WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int kv = WPU == 1 ? warp & 1 : (int)blockIdx.z, hk = WPU == 1 ? 2 * blockIdx.y + (warp >> 1) : (int)blockIdx.y;
+    const int kv = WPU == 1 ? warp & 1 : (int)blockIdx.z, hk = WPU == 1 ? 2 * blockIdx.y + (warp >> 1) : (int)blockIdx.y * a.heads;
     const int t0 = blockIdx.x * a.chunk;
     pdl_wait();
     pdl_launch_dependents();
@@ -302,7 +320,7 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_
     // lane: one row of the chunk.  The rows that are the first of this step in their block lead a unit.
     const int t = t0 + lane;
     int at = 0, n = 0;            // its place in its block; rows of the unit (0: not a leader)
-    int64_t blk = 0;              // the block's number (page, head, block of the page)
+    int64_t blk = 0;              // the block's number with head 0 (page, head, block of the page)
     if (lane < a.chunk && t < a.T) {
         int b;
         Kv8Rows rows;
@@ -326,17 +344,41 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_
                     kv8_report(KV8_BAD_PAGE);
                 } else {
                     n = min(AQ_KV8_BLOCK - at, rows.n - i);
-                    blk = (((int64_t)page * a.Hkv + hk) << a.shift) + (tile & ((1 << a.shift) - 1));
+                    blk = (((int64_t)page * a.Hkv) << a.shift) + (tile & ((1 << a.shift) - 1));
                 }
             }
         }
     }
-    for (unsigned leaders = __ballot_sync(0xffffffffu, n > 0); leaders; leaders &= leaders - 1) {   // (with WPU 4 the same in every warp)
-        const int src = __ffs(leaders) - 1;
-        const int u_at = __shfl_sync(0xffffffffu, at, src), u_n = __shfl_sync(0xffffffffu, n, src);
-        const int64_t u_blk = __shfl_sync(0xffffffffu, blk, src);
-        kw_unit<D, BF16, WPU>(a.x[kv] + (int64_t)(t0 + src) * a.x_row + (int64_t)hk * D, a.x_row, u_n, u_at, a.codes[kv] + u_blk * AQ_KV8_BLOCK * D,
-                              a.scales[kv] + u_blk, WPU == 1 ? 0 : warp, meet);
+    unsigned leaders = __ballot_sync(0xffffffffu, n > 0);   // (with WPU 4 the same in every warp)
+    if (!leaders) return;
+    // (leader, head) pairs in turn, the next one's rows asked for while one is quantised
+    int src = __ffs(leaders) - 1, h = hk;
+    auto load = [&](KwUnit<D, WPU>& u) {
+        const int64_t b = __shfl_sync(0xffffffffu, blk, src) + ((int64_t)h << a.shift);
+        u.load(a.x[kv] + (int64_t)(t0 + src) * a.x_row + (int64_t)h * D, a.x_row, __shfl_sync(0xffffffffu, n, src), __shfl_sync(0xffffffffu, at, src),
+               a.codes[kv] + b * AQ_KV8_BLOCK * D, a.scales[kv] + b, WPU == 1 ? 0 : warp);
+    };
+    auto next = [&] {   // whether there is another pair
+        if (++h < min(hk + a.heads, a.Hkv)) return true;
+        h = hk;
+        leaders &= leaders - 1;
+        src = __ffs(leaders) - 1;
+        return leaders != 0;
+    };
+    KwUnit<D, WPU> u;
+    load(u);
+    for (;;) {
+        if (WPU == 1) {   // (no registers for two)
+            kw_store<D, BF16, WPU>(u, 0, meet);
+            if (!next()) break;
+            load(u);
+        } else {
+            const KwUnit<D, WPU> now = u;
+            const bool more = next();
+            if (more) load(u);
+            kw_store<D, BF16, WPU>(now, warp, meet);
+            if (!more) break;
+        }
     }
 }
 
@@ -345,11 +387,15 @@ static cudaError_t launch_kw(KwArgs& a, cudaStream_t s) {
     // four rows or more per request on average: prompts or chunks of them
     if ((int64_t)a.T >= 4 * (int64_t)a.B) {
         a.chunk = 32;
-        return launch_pdl(kv8_append_kernel<D, BF16, 4>, dim3((unsigned)((a.T + 31) / 32), (unsigned)a.Hkv, 2), dim3(KW_WARPS * 32), 0, s, a);
+        const int64_t blocks = (a.T + 31) / 32;
+        a.heads = 1;   // per CTA: as many as leave each SM several CTAs, so that one's look-ups serve them all
+        while (a.heads < 8 && blocks * 2 * ((a.Hkv + 2 * a.heads - 1) / (2 * a.heads)) >= KW_CTAS * sm_count()) a.heads *= 2;
+        return launch_pdl(kv8_append_kernel<D, BF16, 4>, dim3((unsigned)blocks, (unsigned)((a.Hkv + a.heads - 1) / a.heads), 2), dim3(KW_WARPS * 32), 0, s, a);
     }
     // a decode step's rows are a unit each: a CTA each while there are few
     const int pairs = (a.Hkv + 1) / 2;
     a.chunk = 1;
+    a.heads = 1;
     while (a.chunk < 32 && (int64_t)((a.T + a.chunk - 1) / a.chunk) * pairs > 4 * sm_count()) a.chunk *= 2;
     return launch_pdl(kv8_append_kernel<D, BF16, 1>, dim3((unsigned)((a.T + a.chunk - 1) / a.chunk), (unsigned)pairs), dim3(KW_WARPS * 32), 0, s, a);
 }

@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     constexpr int W = S::WARPS, ROWS = S::ROWS, NV = D / 32;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ KaPiece pieces[2 * W];
-    __shared__ uint32_t sums[W][2];
+    __shared__ uint32_t sums[W][3];
     __shared__ int last_flag[2], group_head[32];
     __shared__ KaSeq seqs[2 * W];   // the requests that a warp's copies and its products are at (kept out of the registers)
     __shared__ KaPiece at_work[W];
@@ -190,19 +190,19 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     pdl_wait();
     pdl_launch_dependents();
     if (lane < 2) pieces[2 * warp + lane].nt = 0;
-    uint32_t total, items;
+    uint32_t total, items, longest;   // of the line: places, items, tiles of the longest item
     KaSeq sq{};
     uint32_t off = 0;             // the run's first place in its request
     uint32_t n_cta, c0 = 0, c1 = 0, x0 = 0, x1 = 0;   // the CTA's share, the warp's run
     Kv8Cut cut{};
+    bool whole_items = false;     // every item belongs to the CTA whose share holds its first place
     auto my_run = [&] {
         n_cta = kv8_ctas(total, items, W, gridDim.x);
         if (blockIdx.x >= n_cta) return;
         cut = kv8_cut(total, n_cta);
         c0 = kv8_begin(cut, blockIdx.x);
         c1 = kv8_begin(cut, blockIdx.x + 1);
-        x0 = kv8_warp_begin(c0, c1, warp, W);
-        x1 = kv8_warp_begin(c0, c1, warp + 1, W);
+        whole_items = longest <= kv8_whole_items(cut, W);
     };
     if (a.B <= 32) {   // a lane per request, in every warp: no warp waits for another
         KaSeq s{};
@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         const uint32_t mine = ka_places(a, s);
         total = __reduce_add_sync(0xffffffffu, mine);
         items = __reduce_add_sync(0xffffffffu, (unsigned)(s.rb * a.Hkv));
+        longest = __reduce_max_sync(0xffffffffu, s.n > 0 ? (unsigned)s.nt : 0u);
         if (total == 0) return;
         uint32_t upto = mine;
 #pragma unroll
@@ -222,6 +223,18 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         }
         my_run();
         if (blockIdx.x >= n_cta) return;
+        if (whole_items) {
+            auto snap = [&](uint32_t x) -> uint32_t {
+                const unsigned at = __ballot_sync(0xffffffffu, upto - mine <= x && x < upto);
+                if (!at) return x;   // (the line's end)
+                const int b = __ffs(at) - 1;
+                return kv8_snap(x, __shfl_sync(0xffffffffu, upto - mine, b), (uint32_t)__shfl_sync(0xffffffffu, s.nt, b) + KV8_ITEM_COST);
+            };
+            c0 = snap(c0);
+            c1 = snap(c1);
+        }
+        x0 = kv8_warp_begin(c0, c1, warp, W);
+        x1 = kv8_warp_begin(c0, c1, warp + 1, W);
         const unsigned here = __ballot_sync(0xffffffffu, upto - mine <= x0 && x0 < upto);
         if (here) {
             const int b = __ffs(here) - 1;
@@ -233,9 +246,10 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     } else {
         uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
         const int per = (a.B + W * 32 - 1) / (W * 32), b0 = threadIdx.x * per;
-        uint32_t mine = 0, my_items = 0;
+        uint32_t mine = 0, my_items = 0, my_longest = 0;
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             const KaSeq s = ka_seq(a, b, ROWS);
+            if (s.n > 0) my_longest = max(my_longest, (uint32_t)s.nt);
             if (s.n > 0 && s.L != __ldg(a.lens + b)) kv8_report(KV8_BAD_LENGTH);
             mine += ka_places(a, s);
             my_items += (uint32_t)s.rb * (uint32_t)a.Hkv;
@@ -246,14 +260,16 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d), w = __shfl_up_sync(0xffffffffu, my_items, d);
             if (lane >= d) { upto += v; my_items += w; }
         }
-        if (lane == 31) { sums[warp][0] = upto; sums[warp][1] = my_items; }
+        my_longest = __reduce_max_sync(0xffffffffu, my_longest);
+        if (lane == 31) { sums[warp][0] = upto; sums[warp][1] = my_items; sums[warp][2] = my_longest; }
         __syncthreads();
         uint32_t before = upto - mine;
-        total = items = 0;
+        total = items = longest = 0;
         for (int w = 0; w < W; ++w) {
             if (w < warp) before += sums[w][0];
             total += sums[w][0];
             items += sums[w][1];
+            longest = max(longest, sums[w][2]);
         }
         if (total == 0) return;
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
@@ -263,6 +279,17 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         my_run();
         if (blockIdx.x >= n_cta) return;
         __syncthreads();
+        if (whole_items) {
+            auto snap = [&](uint32_t x) -> uint32_t {
+                if (x >= total) return x;
+                const int b = kv8_find(marks, a.B, x);
+                return kv8_snap(x, marks[b], (uint32_t)ka_seq(a, b, ROWS).nt + KV8_ITEM_COST);
+            };
+            c0 = snap(c0);
+            c1 = snap(c1);
+        }
+        x0 = kv8_warp_begin(c0, c1, warp, W);
+        x1 = kv8_warp_begin(c0, c1, warp + 1, W);
         if (x0 < x1) {
             const int b = kv8_find(marks, a.B, x0);
             sq = ka_seq(a, b, ROWS);
@@ -817,8 +844,10 @@ cudaError_t launch_kv8_attn(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, co
     uint8_t* sc = reinterpret_cast<uint8_t*>(scratch);
     a.tickets = reinterpret_cast<unsigned*>(sc);
     a.part = sc + KA_TICKET_BYTES;
-    // query rows per pass over a request's keys and values: what it has of them on average
-    const int64_t rows = ((int64_t)a.G * T + a.B - 1) / a.B;
+    // query rows per pass over a request's keys and values: what it has of them; where requests may differ, half as many again as on average
+    // (slots without rows and requests with fewer lie in the average; a second pass over a long request costs more than empty columns)
+    const int64_t each = b.row_start_dev ? (T <= a.B ? 1 : ((int64_t)3 * T + a.B) / (2 * (int64_t)a.B)) : a.n_each;
+    const int64_t rows = a.G * each;
     const int qt = rows <= 4 ? 1 : rows <= 8 || c.head_dim == 256 ? 2 : rows <= 12 ? 3 : 4;
     switch (c.head_dim + qt) {
         case 65: return launch_ka<64, 1>(a, s);

@@ -38,6 +38,15 @@ AQ_HD uint32_t kv8_cta_of(const Kv8Cut& c, uint32_t x) {
     const uint32_t longer = c.more * (c.each + 1u);
     return x < longer ? x / (c.each + 1u) : c.more + (x - longer) / c.each;
 }
+// Whether no item need be shared by CTAs: an item of so many tiles at most makes a CTA's share longer by a few tiles per warp, or by a
+// sixteenth, and spares the merge between CTAs.
+AQ_HD uint32_t kv8_whole_items(const Kv8Cut& c, uint32_t warps) {
+    const uint32_t few = 4u * warps, part = c.each / 16u;
+    return few > part ? few : part;
+}
+// The first item that begins at x or later, of a request whose items begin at `first` and have `len` places each.
+AQ_HD uint32_t kv8_snap(uint32_t x, uint32_t first, uint32_t len) { return first + (x - first + len - 1u) / len * len; }
+
 // First place of warp w of W in a CTA's share [a, e).
 AQ_HD uint32_t kv8_warp_begin(uint32_t a, uint32_t e, uint32_t w, uint32_t W) { return a + (uint32_t)((uint64_t)(e - a) * w / W); }
 

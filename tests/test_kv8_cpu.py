@@ -193,6 +193,8 @@ SRC = textwrap.dedent(r"""
         for (uint32_t d = 1; d <= 256; ++d)
             for (uint32_t x : {0u, 1u, d - 1, d, d + 1, 7 * d - 1, 7 * d, 4095 * d, 4096 * d - 1, 4096 * d})
                 CHECK(kv8_div(x, kv8_magic(d)) == x / d);
+        CHECK(kv8_snap(10, 10, 7) == 10 && kv8_snap(11, 10, 7) == 17 && kv8_snap(17, 10, 7) == 17 && kv8_snap(18, 10, 7) == 24);
+        CHECK(kv8_whole_items(kv8_cut(1000, 10), 8) == 32 && kv8_whole_items(kv8_cut(100000, 10), 8) == 625);
         // rows of a step whatever the caller's array says
         CHECK(kv8_rows(3, 7, 10).first == 3 && kv8_rows(3, 7, 10).n == 4);
         CHECK(kv8_rows(7, 3, 10).n == 0 && kv8_rows(-5, 3, 10).first == 0 && kv8_rows(-5, 3, 10).n == 3);
