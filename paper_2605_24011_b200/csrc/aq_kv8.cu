@@ -80,18 +80,25 @@ __device__ __forceinline__ void kp_scan3(int (&v)[3], int (&tot)[3], int (*sums)
     }
 }
 
-// put(lane's request, j) for j < n: the first FEW by the request's own thread (most requests have one or none), the rest by its warp, 32 at a
-// time.  (A search for the request of each row instead: 4096 rows and 3500 pages of 1000 requests 6.7 us, 8.3 with four searches at once.)
-template <int FEW, typename Fn>
-__device__ __forceinline__ void kp_each(int n, Fn put) {
+// put(lane of a request, j, get(lane, j)) for j < n: the first FEW by the request's own thread (most requests have one or none), the rest by its
+// warp, 32 at a time, four such loads before their stores.  (A search for the request of each row and page instead: 4096 rows and
+// 3500 pages of 1000 requests 6.7 us.)
+template <int FEW, typename Get, typename Put>
+__device__ __forceinline__ void kp_each(int n, Get get, Put put) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int j = 0; j < FEW; ++j)
-        if (j < n) put(lane, j);
+        if (j < n) put(lane, j, get(lane, j));
     for (unsigned left = __ballot_sync(0xffffffffu, n > FEW); left; left &= left - 1) {
         const int src = __ffs(left) - 1, m = __shfl_sync(0xffffffffu, n, src);
-#pragma unroll 4
-        for (int j = FEW + lane; j < m; j += 32) put(src, j);
+        for (int j0 = FEW + lane; j0 < m; j0 += 128) {
+            int v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = j0 + 32 * i < m ? get(src, j0 + 32 * i) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j0 + 32 * i < m) put(src, j0 + 32 * i, v[i]);
+        }
     }
 }
 
@@ -102,9 +109,9 @@ __global__ void __launch_bounds__(KP_THREADS, 1) kv8_plan_kernel(const KpArgs a)
     const int b = threadIdx.x, P = 1 << a.shift;
     pdl_wait();
     pdl_launch_dependents();
-    const int n_free = __ldg(a.n_free);
+    const int n_free = *a.n_free;
     int len = 0, add = 0;
-    if (b < a.B) { len = __ldg(a.lens + b); add = __ldg(a.added + b); }
+    if (b < a.B) { len = a.lens[b]; add = a.added[b]; }
     const int64_t most = a.width << a.shift;
     // -1: the request has ended
     bool ok = len >= 0 && len <= most && add >= -1 && (add < 0 || (int64_t)len + add <= most) && add <= a.n_rows;
@@ -126,7 +133,8 @@ __global__ void __launch_bounds__(KP_THREADS, 1) kv8_plan_kernel(const KpArgs a)
     }
     const int b0 = b & ~31;   // the warp's first request
     // pages of ended requests go on the stack, in the order of the requests and their pages
-    kp_each<0>(add < 0 ? held : 0, [&](int k, int j) { a.free_list[n_free + of[b0 + k].x + j] = __ldg(a.table + (int64_t)(b0 + k) * a.width + j); });
+    kp_each<0>(add < 0 ? held : 0, [&](int k, int j) { return a.table[(int64_t)(b0 + k) * a.width + j]; },
+               [&](int k, int j, int page) { a.free_list[n_free + of[b0 + k].x + j] = page; });
     if (b < a.B) {
         a.lens_out[b] = add < 0 ? 0 : len + add;
         a.row_start[b] = v[2];
@@ -135,14 +143,12 @@ __global__ void __launch_bounds__(KP_THREADS, 1) kv8_plan_kernel(const KpArgs a)
         *a.n_free_out = n_free + tot[0] - tot[1];
         a.row_start[a.B] = tot[2];
     }
-    kp_each<1>(max(add, 0), [&](int k, int j) { a.pos[of[b0 + k].z + j] = length[b0 + k] + j; });
+    kp_each<1>(max(add, 0), [&](int k, int j) { return length[b0 + k] + j; }, [&](int k, int j, int p) { a.pos[of[b0 + k].z + j] = p; });
     for (int i = tot[2] + b; i < a.n_rows; i += KP_THREADS) a.pos[i] = -1;
     __syncthreads();   // (pages that have just been given back may be taken)
     // requests that grow take theirs from the top, in the same order
-    kp_each<1>(grown, [&](int k, int j) {
-        const int4 f = of[b0 + k];
-        a.table[(int64_t)(b0 + k) * a.width + f.w + j] = a.free_list[n_free + tot[0] - 1 - f.y - j];
-    });
+    kp_each<1>(grown, [&](int k, int j) { return a.free_list[n_free + tot[0] - 1 - of[b0 + k].y - j]; },
+               [&](int k, int j, int page) { a.table[(int64_t)(b0 + k) * a.width + of[b0 + k].w + j] = page; });
 }
 
 cudaError_t launch_kv8_plan(const int32_t* lens, const int32_t* added, int n_seqs, int page, int32_t* table, int64_t width, int32_t* free_list,
@@ -210,7 +216,7 @@ struct KwUnit {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int r = i * RPP + sub;
-            v[i] = r < n ? __ldg(reinterpret_cast<const uint4*>(x + r * x_row) + c) : make_uint4(0u, 0u, 0u, 0u);
+            v[i] = r < n ? reinterpret_cast<const uint4*>(x + r * x_row)[c] : make_uint4(0u, 0u, 0u, 0u);
         }
         s_old = at > 0 ? *scale : 0.f;
     }
@@ -313,7 +319,7 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_
     pdl_wait();
     pdl_launch_dependents();
     if (a.row_start) {
-        for (int i = threadIdx.x; i <= a.B; i += KW_WARPS * 32) begin[i] = __ldg(a.row_start + i);
+        for (int i = threadIdx.x; i <= a.B; i += KW_WARPS * 32) begin[i] = a.row_start[i];
         __syncthreads();
     }
     if (hk >= a.Hkv) return;
@@ -333,13 +339,13 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv8_append_kernel(const __grid_
         }
         const int i = t - rows.first;
         if (i >= 0 && i < rows.n) {
-            const int64_t pos = (int64_t)__ldg(a.lens + b) - rows.n + i;
+            const int64_t pos = (int64_t)a.lens[b] - rows.n + i;
             at = (int)(pos & (AQ_KV8_BLOCK - 1));
             const int64_t tile = pos >> 5, pg = tile >> a.shift;
             if (pos < 0 || pg >= a.width) {
                 kv8_report(KV8_BAD_LENGTH);
             } else if (i == 0 || at == 0) {
-                const int page = __ldg(a.table + (int64_t)b * a.width + pg);
+                const int page = a.table[(int64_t)b * a.width + pg];
                 if (page < 0 || page >= a.n_pages) {
                     kv8_report(KV8_BAD_PAGE);
                 } else {

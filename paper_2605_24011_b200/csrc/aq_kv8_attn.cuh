@@ -123,11 +123,11 @@ struct KaSeq {
 __device__ __forceinline__ KaSeq ka_seq(const KaArgs& a, int b, int rows) {
     KaSeq s;
     s.b = b;
-    const Kv8Rows r = a.row_start ? kv8_rows(__ldg(a.row_start + b), __ldg(a.row_start + b + 1), a.T) : Kv8Rows{b * a.n_each, a.n_each};
+    const Kv8Rows r = a.row_start ? kv8_rows(a.row_start[b], a.row_start[b + 1], a.T) : Kv8Rows{b * a.n_each, a.n_each};
     s.row0 = r.first;
     s.n = r.n;
     const int64_t most = a.width << (a.shift + 5);
-    s.L = (int)min((int64_t)max(__ldg(a.lens + b), 0), most);
+    s.L = (int)min((int64_t)max(a.lens[b], 0), most);
     s.nt = max(1, (s.L + KA_TILE - 1) / KA_TILE);   // (a request without positions has one tile that is not read: its rows become 0)
     s.rb = (s.n * a.G + rows - 1) / rows;   // (n G <= 2^20)
     return s;
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         KaSeq s{};
         if (lane < a.B) {
             s = ka_seq(a, lane, ROWS);
-            if (s.n > 0 && s.L != __ldg(a.lens + lane)) kv8_report(KV8_BAD_LENGTH);
+            if (s.n > 0 && s.L != a.lens[lane]) kv8_report(KV8_BAD_LENGTH);
         }
         const uint32_t mine = ka_places(a, s);
         total = __reduce_add_sync(0xffffffffu, mine);
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             const KaSeq s = ka_seq(a, b, ROWS);
             if (s.n > 0) my_longest = max(my_longest, (uint32_t)s.nt);
-            if (s.n > 0 && s.L != __ldg(a.lens + b)) kv8_report(KV8_BAD_LENGTH);
+            if (s.n > 0 && s.L != a.lens[b]) kv8_report(KV8_BAD_LENGTH);
             mine += ka_places(a, s);
             my_items += (uint32_t)s.rb * (uint32_t)a.Hkv;
         }
@@ -352,8 +352,8 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                                         (int64_t)(hk * a.G + (r - tok * a.G)) * D + 4 * t;
 #pragma unroll
                     for (int c = 0; c < D / 32; ++c) {
-                        raw[u][c][0] = __ldg(reinterpret_cast<const uint2*>(q + 32 * c));
-                        raw[u][c][1] = __ldg(reinterpret_cast<const uint2*>(q + 32 * c + 16));
+                        raw[u][c][0] = *reinterpret_cast<const uint2*>(q + 32 * c);
+                        raw[u][c][1] = *reinterpret_cast<const uint2*>(q + 32 * c + 16);
                     }
                 } else {
 #pragma unroll
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 if (p_page0 < 0 || pg >= p_page0 + 32 || pg < p_page0) {
                     p_page0 = pg;
                     const int i = pg + lane;
-                    p_pages = (int64_t)i < a.width && (i << (a.shift + 5)) < ps.L ? __ldg(a.table + (int64_t)ps.b * a.width + i) : -1;
+                    p_pages = (int64_t)i < a.width && (i << (a.shift + 5)) < ps.L ? a.table[(int64_t)ps.b * a.width + i] : -1;
                 }
                 const int page = __shfl_sync(0xffffffffu, p_pages, pg - p_page0);
                 p_ok = page >= 0 && page < a.n_pages;

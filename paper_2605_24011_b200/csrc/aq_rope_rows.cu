@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(RR_THREADS, RR_CTAS) rope_rows_kernel(const __
     constexpr int PPU = TWO ? N : N / 2;   // pairs per unit
     for (int i = threadIdx.x; i < n_rows * half; i += RR_THREADS) {
         const int r = i / half, k = i - r * half;
-        const double turn = (double)__ldg(a.pos + row0 + r) * a.turns[k];
+        const double turn = (double)a.pos[row0 + r] * a.turns[k];
         float s, c;
         sincospif((float)(2.0 * (turn - rint(turn))), &s, &c);
         table[r * half + k % PPU * a.turned + k / PPU] = make_float2(c * a.magnitude, s * a.magnitude);
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(RR_THREADS, RR_CTAS) rope_rows_kernel(const __
             const bool turned = u < a.turned;
             lo[k] = turned ? (HALF || N > 1 ? u * N : 2 * u) : a.rot + (u - a.turned) * N;
             angle[k] = turned ? dr * half + u : -1;
-            if (i0 + k * RR_THREADS >= n || __ldg(a.pos + row0 + dr) < 0) angle[k] = -2;
+            if (i0 + k * RR_THREADS >= n || a.pos[row0 + dr] < 0) angle[k] = -2;
             va[k].load(x + lo[k]);
             if (TWO) vb[TWO ? k : 0].load(x + (turned ? lo[k] + (HALF ? half : 1) : lo[k]));
         }
