@@ -204,6 +204,11 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         c1 = kv8_begin(cut, blockIdx.x + 1);
         whole_items = longest <= kv8_whole_items(cut, W);
     };
+    auto cut_warps = [&] {   // (the places in front of the first tile of a share that begins with an item are no warp's work)
+        const uint32_t a0 = whole_items ? min(c0 + KV8_ITEM_COST, c1) : c0;
+        x0 = kv8_warp_begin(a0, c1, warp, W);
+        x1 = kv8_warp_begin(a0, c1, warp + 1, W);
+    };
     if (a.B <= 32) {   // a lane per request, in every warp: no warp waits for another
         KaSeq s{};
         if (lane < a.B) {
@@ -233,8 +238,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             c0 = snap(c0);
             c1 = snap(c1);
         }
-        x0 = kv8_warp_begin(c0, c1, warp, W);
-        x1 = kv8_warp_begin(c0, c1, warp + 1, W);
+        cut_warps();
         const unsigned here = __ballot_sync(0xffffffffu, upto - mine <= x0 && x0 < upto);
         if (here) {
             const int b = __ffs(here) - 1;
@@ -288,8 +292,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             c0 = snap(c0);
             c1 = snap(c1);
         }
-        x0 = kv8_warp_begin(c0, c1, warp, W);
-        x1 = kv8_warp_begin(c0, c1, warp + 1, W);
+        cut_warps();
         if (x0 < x1) {
             const int b = kv8_find(marks, a.B, x0);
             sq = ka_seq(a, b, ROWS);
