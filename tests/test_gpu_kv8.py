@@ -321,6 +321,26 @@ def test_attention_many_requests(aq):
     _check_attn(aq, lens[:300], 1, 2, 128, 32, rows=[int(v) for v in g.integers(0, 4, 300)], seed=6, outs=("f16",))
 
 
+@pytest.mark.parametrize("Hkv,G,D,rows", ((8, 4, 128, 1), (8, 4, 128, 2), (8, 4, 128, 3), (8, 4, 128, 4), (6, 3, 64, 5), (5, 8, 256, 1), (5, 2, 256, 1), (9, 5, 64, 2)))
+def test_attention_runs_over_several_items(aq, Hkv, G, D, rows):
+    # items shared by CTAs and warps, runs that end one and begin the next, for every number of query rows per pass
+    lens = [2100, 1999, 2500, 31, 1900, 2222]
+    _check_attn(aq, lens, Hkv, G, D, 128, rows=[rows] * len(lens), seed=rows + D, outs=("f32",), tail=1)
+
+
+def test_attention_many_requests_with_long_ones_among_them(aq):
+    g = np.random.default_rng(15)
+    lens = [int(v) for v in g.integers(0, 300, 60)]
+    lens[7], lens[41], lens[59] = 7000, 5003, 4097
+    _check_attn(aq, lens, 2, 2, 64, 64, seed=15, outs=("f32",))
+    _check_attn(aq, lens, 2, 2, 128, 64, rows=[min(L, int(v)) for L, v in zip(lens, g.integers(0, 9, 60))], seed=16, outs=("f32",))
+
+
+def test_attention_more_rows_than_a_pass_takes(aq):
+    _check_attn(aq, [5000, 40, 2200], 1, 4, 128, 128, rows=[40, 2, 1], seed=17, outs=("f32",))
+    _check_attn(aq, [3000, 40], 2, 8, 256, 64, rows=[5, 3], seed=18, outs=("f32",))
+
+
 def test_attention_a_prompt(aq):
     _check_attn(aq, [150, 70], 2, 2, 128, 64, rows=[150, 33], seed=8, outs=("f32",))
 
@@ -559,6 +579,72 @@ def test_append_pages_outside_the_pool_are_not_written(aq):
             aq.aq_check()
         assert e.value.status == aq.AQ_ERR_RANGE
         assert torch.equal(s.cache.k, kept[0]) and torch.equal(s.cache.v, kept[1])
+
+
+# ---- the binding ---------------------------------------------------------------------------------------------------
+def test_calls_on_a_stream_of_the_callers(aq):
+    """stream=: behind what that stream has before, whatever torch's current stream is."""
+    side = torch.cuda.Stream()
+    s = Served(aq, [900, 40], 2, 128, 64, 80)
+    b, q = s.batch(aq), torch.randn(2, 8, 128).half()
+    want, tol = _attn_reference(s, q.double().numpy(), [1, 1], 0.0)
+    qd, late = q.cuda(), torch.zeros(2, 8, 128, dtype=torch.float16, device="cuda")
+    out, scratch = torch.zeros(2, 8, 128, device="cuda"), aq.aq_kv8_scratch()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        late.copy_(qd)
+    aq.aq_kv8_attn(s.cache, b, late, out, scratch, stream=side)
+    side.synchronize()
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol * 1.01)
+    # the other calls
+    k = torch.randn(2, 2, 128).half()
+    later = torch.zeros_like(k, device="cuda")
+    kd = k.cuda()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        later.copy_(kd)
+    aq.aq_rope_rows(aq.aq_rope_setup(128), later, _i32([3, 0]), stream=side.cuda_stream)
+    aq.aq_kv8_append(s.cache, b, later, later, stream=side.cuda_stream)
+    aq.aq_check(side)
+    turned = O.rope_rows(k.double().numpy(), [3, 0], O.rope_frequencies(128), "half")
+    assert np.all(np.abs(later.double().cpu().numpy() - turned) <= 2.0 ** -20 * 8 + 2.0 ** -11 * np.abs(turned))
+    now = O.append(s.k.numpy(), s.ks.numpy(), s.v.numpy(), s.vs.numpy(), [900, 40], [0, 1, 2], s.table, later.float().cpu().numpy(), later.float().cpu().numpy())
+    for got, w in zip((s.cache.k, s.cache.k_scale, s.cache.v, s.cache.v_scale), now):
+        assert np.array_equal(got.cpu().numpy(), w, equal_nan=w.dtype.kind == "f")
+
+
+def test_binding_refuses(aq):
+    s = Served(aq, [90, 40], 2, 128, 64, 81)
+    b, q = s.batch(aq), torch.zeros(2, 8, 128, dtype=torch.float16, device="cuda")
+    out, scratch = torch.zeros_like(q), aq.aq_kv8_scratch()
+    k = torch.zeros(2, 2, 128, dtype=torch.float16, device="cuda")
+    i, pos, rope = _i32([1, 2]), _i32([5, 6]), aq.aq_rope_setup(128)
+    attn = lambda **kw: aq.aq_kv8_attn(**{**dict(cache=s.cache, batch=b, q=q, out=out, scratch=scratch), **kw})
+    append = lambda **kw: aq.aq_kv8_append(**{**dict(cache=s.cache, batch=b, k=k, v=k), **kw})
+    turn = lambda **kw: aq.aq_rope_rows(**{**dict(rope=rope, x=q, pos=pos, out=out), **kw})
+    plan = lambda **kw: aq.aq_kv8_plan(**{**dict(lens=i, new=i, table=_i32([[0, 1], [2, 3]]), free=i, n_free=_i32([2]), page=64, lens_out=i, n_free_out=_i32([2]),
+                                                 row_start=_i32([0, 1, 2]), pos=pos), **kw})
+    bad = [lambda: attn(q=q.cpu()), lambda: attn(q=q.float()[:, :, :64].half()), lambda: attn(q=q[:, ::2]), lambda: attn(q=q[0]), lambda: attn(out=out[:1]),
+           lambda: attn(scratch=scratch.cpu()), lambda: attn(q=q.int()), lambda: append(k=k[:, :1]), lambda: append(v=k.bfloat16()), lambda: append(k=k.transpose(0, 1)),
+           lambda: append(v=torch.zeros(2, 3, 128, dtype=torch.float16, device="cuda")[:, :2]), lambda: turn(pos=pos.long()), lambda: turn(pos=pos[:1]),
+           lambda: turn(out=out[:, :4]), lambda: turn(x=[1]), lambda: plan(lens=i.long()), lambda: plan(new=_i32([1])), lambda: plan(pos=_i32([1, 2, 3, 4])[::2]),
+           lambda: plan(table=i), lambda: plan(n_free=i), lambda: plan(row_start=i), lambda: aq.Kv8Cache(s.cache.k[:, :, ::2], s.cache.v, s.cache.k_scale, s.cache.v_scale),
+           lambda: aq.Kv8Cache(s.cache.k.float(), s.cache.v, s.cache.k_scale, s.cache.v_scale), lambda: aq.Kv8Batch(b.lens.long(), b.table),
+           lambda: aq.Kv8Batch(b.lens, b.table.t()[:1].t())]
+    for n, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            raise AssertionError(n)
+    for n, (call, status) in enumerate(((lambda: attn(scratch=scratch[:100]), aq.AQ_ERR_INVALID_ARG), (lambda: attn(q=q[:, :7], out=out[:, :7]), aq.AQ_ERR_INVALID_ARG),
+                                        (lambda: attn(q=q.float(), out=out.float()), aq.AQ_ERR_UNSUPPORTED), (lambda: plan(page=48), aq.AQ_ERR_INVALID_ARG),
+                                        (lambda: turn(out=out.float()), aq.AQ_ERR_UNSUPPORTED), (lambda: turn(rope=aq.aq_rope_setup(256)), aq.AQ_ERR_INVALID_ARG),
+                                        (lambda: append(k=k.float(), v=k.float()), aq.AQ_ERR_UNSUPPORTED))):
+        with pytest.raises(aq.AqError) as e:
+            call()
+        assert e.value.status == status, n
+    aq.aq_check()
 
 
 # ---- together ------------------------------------------------------------------------------------------------------
