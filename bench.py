@@ -233,6 +233,23 @@ def run_micro(args):
         fn = lambda i: aq.aq_attn_decode(q, caches[i % n_copies][0], caches[i % n_copies][1], L, y, scratch)
         work, unit = per, "GB/s"
         out.update({"heads": H, "kv_heads": Hkv, "L": L, "copies": n_copies})
+    elif args.micro == "kv8_attn":
+        # one token each of 32 requests of --K positions against a paged 8-bit cache (--N key/value heads of 128, 32 query heads); bytes per
+        # call: the codes and scales of all positions; inputs larger than L2 (--K 4096: 269 MB)
+        L, Hkv, B, page = args.K or 4096, args.N or 8, 32, 64
+        g = torch.Generator(device="cuda")
+        g.manual_seed(12)
+        n = B * -(-L // page)
+        codes = [torch.randint(-127, 128, (n, Hkv, page, 128), generator=g, device="cuda", dtype=torch.int8) for _ in range(2)]
+        scales = [torch.rand((n, Hkv, page // 32), generator=g, device="cuda") * 0.03 for _ in range(2)]
+        cache = aq.Kv8Cache(codes[0], codes[1], scales[0], scales[1])
+        table = torch.randperm(n, generator=g, device="cuda").to(torch.int32).view(B, -1)
+        batch = aq.Kv8Batch(torch.full((B,), L, dtype=torch.int32, device="cuda"), table)
+        q = torch.randn((B, 32, 128), generator=g, device="cuda", dtype=torch.float16)
+        y, scratch = torch.empty_like(q), aq.aq_kv8_scratch()
+        fn = lambda i: aq.aq_kv8_attn(cache, batch, q, y, scratch)
+        work, unit = 2 * B * Hkv * (L * 128 + 4 * -(-L // 32)), "GB/s"
+        out.update({"requests": B, "heads": 32, "kv_heads": Hkv, "L": L, "page": page})
     elif args.micro in ("decode_linear", "prefill_linear", "dequant"):
         decode = args.micro == "decode_linear"
         M = args.M or (1 if decode else 512)
@@ -277,7 +294,7 @@ def run_micro(args):
     aq.aq_check()
     ms = e0.elapsed_time(e1) / args.steps
     out.update({"us_per_call": 1e3 * ms, "value": work / (ms * 1e-3) / (1e9 if unit == "GB/s" else 1e12), "unit": unit})
-    if args.micro == "attn_decode":
+    if args.micro in ("attn_decode", "kv8_attn"):
         # the same calls recorded once into a CUDA graph and replayed: device time without the host's per-call cost
         n = max(16, min(args.steps, 64))
         side = torch.cuda.Stream()
@@ -492,7 +509,7 @@ def main():
     ap.add_argument("--impl", default="ours", choices=("ours", "reference"))
     ap.add_argument("--layers", type=int, default=32, help="decoder layers (32 = the full workload)")
     ap.add_argument("--no-extras", action="store_true", help="skip prefill / dequant / oracle legs")
-    ap.add_argument("--micro", choices=("decode_linear", "prefill_linear", "dequant", "decode_stack", "prefill_stack", "pack", "pack_opt", "rbf_gram", "hsic", "attn_decode", "decode_token"),
+    ap.add_argument("--micro", choices=("decode_linear", "prefill_linear", "dequant", "decode_stack", "prefill_stack", "pack", "pack_opt", "rbf_gram", "hsic", "attn_decode", "kv8_attn", "decode_token"),
                     help="time one kernel on a small case (the command ncu captures are taken from) instead of the benchmark")
     ap.add_argument("--configs", action="store_true",
                     help="time all five workload configurations once each and print one JSON object (not the benchmark line)")

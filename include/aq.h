@@ -269,6 +269,10 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
  * positions (off by 2^-17 of that) and are summed as rounded, sums over positions are binary32: against the exact result for the
  * cached values an output is off by at most about 2^-12 (sum_p softmax_p |V[p]| + what that sum would be with every |V[p]| at its block's
  * largest), the scores' part and its own rounding.  A query row with a NaN or an infinity gives NaN.
+ * Sums go in a fixed order: the same call gives the same bits.
+ * Errors of the aq_kv8 calls: AQ_ERR_INVALID_ARG (null / misaligned pointer, a size outside the ranges above, a stride that is no multiple of 8 or
+ * shorter than a row, a scratch that is too small), AQ_ERR_UNSUPPORTED (head_dim, dtype, more than 256 key/value heads, more than 256 query heads for
+ * one, more than AQ_KV8_MAX_SEQS requests, a step that could be of 2^31 tiles of 32 positions), AQ_ERR_ARCH, AQ_ERR_CUDA.
  */
 aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* q_dev, int64_t q_stride, void* out_dev,
                         int64_t out_stride, int64_t n_rows, int n_heads, float scale, aq_dtype_t dtype, aq_dtype_t out_dtype, void* scratch_dev,

@@ -17,10 +17,15 @@
 //       product with ones: the normaliser sums what the values are weighted with.
 //   O = al O + vs fac (256 hi + lo) in binary32; ldmatrix.trans on pairs of bytes gives dims 2g, 2g + 1 of two positions per register.
 // A NaN (of a scale, of a query row) travels in the scales: F, fac.
-// Every warp has a contiguous run of the line of tiles (aq_kv8_runs.h) and streams it through its own cp.async ring without
-// waiting for another warp; runs differ by one tile at most whatever the requests' lengths are.  What a warp finishes alone it
-// writes; pieces of an item are merged over the warps of the CTA in shared memory, then over the CTAs in the scratch by the last
-// CTA to arrive (tickets; nobody waits).
+// Every warp has a contiguous run of the line (aq_kv8_runs.h) and streams it through its own cp.async ring without waiting for another
+// warp; runs differ by one place at most whatever the requests' lengths are.  What a warp finishes alone it writes; pieces of an item are merged
+// over the warps of the CTA in shared memory, then over the CTAs in the scratch by the last CTA to arrive (counters; nobody waits), in two
+// levels above 14 CTAs.  All sums go in a fixed order.  Where items are short a CTA's share is moved to whole ones.
+// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 54.4 us, 4.9 TB/s, 0.75 of the copy rate (a third of the time is
+// the unequal speed of the SMs, the first trips and the merges); one request of 512 positions, 32 heads: 7.8 us; 100001 positions, 8 heads of 256 on
+// 1: 24.9 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows): 70 us for 296 MB, bound by issue slots.
+// Fewer warps are slower where the arithmetic counts (61 ragged requests: 76 us with 8), more do not fit the registers (168 each
+// with 12: with the walks' state in them 148 us).
 // (Included by aq_kv8.cu alone, which has the status word and the host calls.)
 #pragma once
 
@@ -457,7 +462,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     most = max(most & 0xffffu, most >> 16);
                     const bool poison = most >= (a.q_bf16 ? 0x7f80u : 0x7c00u);
                     const float big = a.q_bf16 ? __uint_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
-                    const float up = poison ? 0.f : fminf(__fdividef(32638.9f, big), 3e38f);   // (rows of zeros: 0 times the largest number)
+                    const float up = poison ? 0.f : fminf(32639.f / big, 3e38f);   // (rows of zeros: 0 times the largest number)
                     // q up + 1.5 * 2^23 has rint(q up) in its low bits; 128 more, and the second byte is the high plane's
                     const float magic = 12582912.f + ((g & 1) ? 0.f : 128.f);
                     const uint32_t pick = (g & 1) ? 0x0040 : 0x0051;
@@ -486,7 +491,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                             }
                     }
                     // of the query row whose scores this lane holds (row t of the group: lanes of columns 2t and 2t + 1 have it)
-                    const float step = poison ? __uint_as_float(0x7fc00000u) : __fdividef(big, 32638.9f);
+                    const float step = poison ? __uint_as_float(0x7fc00000u) : big * (1.f / 32639.f);
                     fq[u] = __shfl_sync(0xffffffffu, step, 8 * t) * a.scale_log2;
                     lim[u] = sq.L - sq.n + (int)kv8_div((uint32_t)min(pc.q0 + 4 * u + t, pc.rows - 1), a.G_magic) + 1;   // positions before this one are seen
                     m[u] = -INFINITY;
