@@ -259,7 +259,8 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
  * aq_kv8_attn -- out[t][h] = softmax_p(scale * q[t][h] . K[p]) V[p] over the cached positions p of row t's request up to its own;
  * query head h reads key/value head h / (n_heads / n_kv_heads).  A row that sees no position is 0.
  *   q_dev   : DEVICE, rows of [n_heads][head_dim] of `dtype` (AQ_F16 / AQ_BF16), 16-byte aligned, q_stride elements (a multiple of 8) apart
- *   out_dev : DEVICE, rows of [n_heads][head_dim] of out_dtype (any of the three), 16-byte aligned, out_stride elements (a multiple of 8) apart
+ *   out_dev : DEVICE, rows of [n_heads][head_dim] of out_dtype (any of the three), 16-byte aligned, out_stride elements (a multiple of 8) apart;
+ *             not q_dev, nor in its way
  *   scale   : <= 0 means 1 / sqrt(head_dim)
  *   scratch_dev : DEVICE, 256-byte aligned, AQ_KV8_SCRATCH_BYTES, ZERO before its first use; a call leaves it as the next one wants it.
  *             Calls that may overlap in time (streams, captured graphs) need scratch of their own.

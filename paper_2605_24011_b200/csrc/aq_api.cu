@@ -523,8 +523,8 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
 aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch, const void* q_dev, int64_t q_stride, void* out_dev,
                         int64_t out_stride, int64_t n_rows, int n_heads, float scale, aq_dtype_t dtype, aq_dtype_t out_dtype, void* scratch_dev,
                         size_t scratch_bytes, aq_stream_t stream) {
-    if (!q_dev || !out_dev || !scratch_dev || !aligned16(q_dev) || !aligned16(out_dev) || (reinterpret_cast<uintptr_t>(scratch_dev) & 255u) ||
-        !std::isfinite(scale))
+    if (!q_dev || !out_dev || q_dev == out_dev || !scratch_dev || !aligned16(q_dev) || !aligned16(out_dev) ||
+        (reinterpret_cast<uintptr_t>(scratch_dev) & 255u) || !std::isfinite(scale))
         return AQ_ERR_INVALID_ARG;
     if (dtype != AQ_F16 && dtype != AQ_BF16) return (dtype == AQ_F32) ? AQ_ERR_UNSUPPORTED : AQ_ERR_INVALID_ARG;
     if (out_dtype != AQ_F16 && out_dtype != AQ_BF16 && out_dtype != AQ_F32) return AQ_ERR_INVALID_ARG;

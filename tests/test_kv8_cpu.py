@@ -65,7 +65,7 @@ def test_attention_refuses(aq):
     lib = aq.raw_lib()
     big = aq.AQ_KV8_SCRATCH_BYTES
 
-    def call(c=None, b=None, q=FAKE, qs=4096, out=FAKE, os_=4096, rows=8, heads=32, scale=0.0, dt=aq.AQ_F16, odt=aq.AQ_F32, sc=FAKE, n=big):
+    def call(c=None, b=None, q=FAKE, qs=4096, out=2 * FAKE, os_=4096, rows=8, heads=32, scale=0.0, dt=aq.AQ_F16, odt=aq.AQ_F32, sc=FAKE, n=big):
         c, b = _cache(aq, **(c or {})), _batch(aq, **(b or {}))
         return lib.aq_kv8_attn(C.byref(c), C.byref(b), q, qs, out, os_, rows, heads, scale, dt, odt, sc, n, None)
     for c in BAD_CACHE:
@@ -74,7 +74,7 @@ def test_attention_refuses(aq):
         assert call(b=b) == aq.AQ_ERR_INVALID_ARG, b
     for c, b in UNSUPPORTED:
         assert call(c=c, b=b, heads=257, qs=1 << 20, os_=1 << 20) == aq.AQ_ERR_UNSUPPORTED, (c, b)
-    for kw in (dict(q=0), dict(out=0), dict(sc=0), dict(q=FAKE + 4), dict(out=FAKE + 8), dict(sc=FAKE + 128), dict(n=big - 1), dict(heads=33), dict(heads=0),
+    for kw in (dict(q=0), dict(out=0), dict(out=FAKE), dict(sc=0), dict(q=FAKE + 4), dict(out=FAKE + 8), dict(sc=FAKE + 128), dict(n=big - 1), dict(heads=33), dict(heads=0),
                dict(qs=4092), dict(qs=4088), dict(os_=4094), dict(os_=4088), dict(rows=0), dict(rows=4097), dict(dt=5), dict(odt=5),
                dict(scale=float("inf")), dict(scale=float("nan"))):
         assert call(**kw) == aq.AQ_ERR_INVALID_ARG, kw
