@@ -41,11 +41,11 @@ def _compile(src):
     return obj
 
 
-def _compile_torch():
+def _compile_torch(force: bool = False):
     """_aq_torch.so, against the torch that this interpreter has (its headers and libraries, no others)."""
     src = os.path.join(CSRC, "aq_torch.cpp")
     deps = max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "aq.h")))
-    if os.path.exists(TORCH_OUT) and os.path.getmtime(TORCH_OUT) >= deps:
+    if not force and os.path.exists(TORCH_OUT) and os.path.getmtime(TORCH_OUT) >= deps:
         return
     import sysconfig
 
@@ -67,7 +67,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return OUT
     os.makedirs(OBJ, exist_ok=True)
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
-        binding = ex.submit(_compile_torch)
+        binding = ex.submit(_compile_torch, force)
         objs = list(ex.map(_compile, _sources()))
         binding.result()
     cmd = [NVCC, "-shared", "-o", OUT, *objs, "-cudart", "static"]

@@ -181,7 +181,7 @@ __device__ __forceinline__ bool ka_arrive(unsigned* ticket, unsigned one, unsign
 template <int D, int QT>
 __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel(const __grid_constant__ KaArgs a) {
     using S = KaShape<D, QT>;
-    constexpr int W = S::WARPS, ROWS = S::ROWS, NV = D / 32;
+    constexpr int W = S::WARPS, ROWS = S::ROWS;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ KaPiece pieces[2 * W];
     __shared__ uint32_t sums[W][3];
