@@ -196,7 +196,8 @@ aq_status_t aq_attn_decode(const void* q_dev, const void* k_cache_dev, const voi
  *
  * What these device arrays say cannot be checked on the host.  A page outside the pool, or a length that does not fit the table,
  * is not followed: such positions count as masked (append: are not written), and the next aq_check on that device returns
- * AQ_ERR_RANGE.
+ * AQ_ERR_RANGE.  Row marks are held inside the step; where they descend so that requests have more than n_rows rows between them,
+ * aq_kv8_attn writes nothing, with the same report.
  */
 #define AQ_KV8_BLOCK 32
 #define AQ_KV8_MAX_SEQS 1024
@@ -266,7 +267,7 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
  *             Calls that may overlap in time (streams, captured graphs) need scratch of their own.
  * Built for decode (a few new tokens per request against long contexts); more rows per request are right but re-read the cache
  * for every 8 (head_dim 256) or 16 of a head's query rows.  A query row enters the products in 16 bits against its largest magnitude (off by
- * 2^-16 of it at most), the products with the codes are exact, weights enter the second product in 16 bits against the largest of their 32
+ * 2^-16 of it at most; bfloat16 rows under 2^-113: by 2^-128), the products with the codes are exact, weights enter the second product in 16 bits against the largest of their 32
  * positions (off by 2^-17 of that) and are summed as rounded, sums over positions are binary32: against the exact result for the
  * cached values an output is off by at most about 2^-12 (sum_p softmax_p |V[p]| + what that sum would be with every |V[p]| at its block's
  * largest), the scores' part and its own rounding.  A query row with a NaN or an infinity gives NaN.

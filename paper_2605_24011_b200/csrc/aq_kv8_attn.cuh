@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     constexpr int W = S::WARPS, ROWS = S::ROWS;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ KaPiece pieces[2 * W];
-    __shared__ uint32_t sums[W][3];
+    __shared__ uint32_t sums[W][4];
     __shared__ int last_flag[2], group_head[32];
     __shared__ KaSeq seqs[2 * W];   // the requests that a warp's copies and its products are at (kept out of the registers)
     __shared__ KaPiece at_work[W];
@@ -214,6 +214,13 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         x0 = kv8_warp_begin(a0, c1, warp, W);
         x1 = kv8_warp_begin(a0, c1, warp + 1, W);
     };
+    // Row marks that descend can name more rows than the step has, and the line would be longer than the host could know (it counts in 32
+    // bits): such a step is not followed.
+    auto too_many = [&](uint32_t rows) {
+        if (rows <= (uint32_t)a.T) return false;
+        if (blockIdx.x == 0 && threadIdx.x == 0) kv8_report(KV8_BAD_LENGTH);
+        return true;
+    };
     if (a.B <= 32) {   // a lane per request, in every warp: no warp waits for another
         KaSeq s{};
         if (lane < a.B) {
@@ -224,7 +231,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         total = __reduce_add_sync(0xffffffffu, mine);
         items = __reduce_add_sync(0xffffffffu, (unsigned)(s.rb * a.Hkv));
         longest = __reduce_max_sync(0xffffffffu, s.n > 0 ? (unsigned)s.nt : 0u);
-        if (total == 0) return;
+        if (total == 0 || too_many(__reduce_add_sync(0xffffffffu, (unsigned)s.n))) return;
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -255,12 +262,13 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     } else {
         uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
         const int per = (a.B + W * 32 - 1) / (W * 32), b0 = threadIdx.x * per;
-        uint32_t mine = 0, my_items = 0, my_longest = 0;
+        uint32_t mine = 0, my_items = 0, my_longest = 0, my_rows = 0;
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             const KaSeq s = ka_seq(a, b, ROWS);
             if (s.n > 0) my_longest = max(my_longest, (uint32_t)s.nt);
             if (s.n > 0 && s.L != a.lens[b]) kv8_report(KV8_BAD_LENGTH);
             mine += ka_places(a, s);
+            my_rows += (uint32_t)s.n;
             my_items += (uint32_t)s.rb * (uint32_t)a.Hkv;
         }
         uint32_t upto = mine;
@@ -270,17 +278,20 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             if (lane >= d) { upto += v; my_items += w; }
         }
         my_longest = __reduce_max_sync(0xffffffffu, my_longest);
-        if (lane == 31) { sums[warp][0] = upto; sums[warp][1] = my_items; sums[warp][2] = my_longest; }
+        my_rows = __reduce_add_sync(0xffffffffu, my_rows);
+        if (lane == 31) { sums[warp][0] = upto; sums[warp][1] = my_items; sums[warp][2] = my_longest; sums[warp][3] = my_rows; }
         __syncthreads();
         uint32_t before = upto - mine;
         total = items = longest = 0;
+        uint32_t rows = 0;
         for (int w = 0; w < W; ++w) {
             if (w < warp) before += sums[w][0];
             total += sums[w][0];
             items += sums[w][1];
             longest = max(longest, sums[w][2]);
+            rows += sums[w][3];
         }
-        if (total == 0) return;
+        if (total == 0 || too_many(rows)) return;
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             marks[b] = before;
             before += ka_places(a, ka_seq(a, b, ROWS));
@@ -462,7 +473,8 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     most = max(most & 0xffffu, most >> 16);
                     const bool poison = most >= (a.q_bf16 ? 0x7f80u : 0x7c00u);
                     const float big = a.q_bf16 ? __uint_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
-                    const float up = poison ? 0.f : fminf(32639.f / big, 3e38f);   // (rows of zeros: 0 times the largest number)
+                    // (a row under 1.1e-34, which bfloat16 can hold, is in steps of 1 / 3e38; rows of zeros are too)
+                    const float up = poison ? 0.f : fminf(32639.f / big, 3e38f);
                     // q up + 1.5 * 2^23 has rint(q up) in its low bits; 128 more, and the second byte is the high plane's
                     const float magic = 12582912.f + ((g & 1) ? 0.f : 128.f);
                     const uint32_t pick = (g & 1) ? 0x0040 : 0x0051;
@@ -491,7 +503,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                             }
                     }
                     // of the query row whose scores this lane holds (row t of the group: lanes of columns 2t and 2t + 1 have it)
-                    const float step = poison ? __uint_as_float(0x7fc00000u) : big * (1.f / 32639.f);
+                    const float step = poison ? __uint_as_float(0x7fc00000u) : up < 3e38f ? big * (1.f / 32639.f) : 1.f / 3e38f;
                     fq[u] = __shfl_sync(0xffffffffu, step, 8 * t) * a.scale_log2;
                     lim[u] = sq.L - sq.n + (int)kv8_div((uint32_t)min(pc.q0 + 4 * u + t, pc.rows - 1), a.G_magic) + 1;   // positions before this one are seen
                     m[u] = -INFINITY;

@@ -429,6 +429,47 @@ def test_attention_pages_outside_the_pool_are_not_followed(aq):
     assert bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("n", (3, 41))
+def test_attention_row_marks_that_name_too_many_rows(aq, n):
+    """Marks that descend: requests that have more rows between them than the step has.  Nothing is written."""
+    s = Served(aq, [100] * n, 2, 128, 32, 17)
+    q = torch.randn(2, 4, 128).half().cuda()
+    out = torch.full((2, 4, 128), float("nan"), dtype=torch.float32, device="cuda")
+    scratch = aq.aq_kv8_scratch()
+    aq.aq_kv8_attn(s.cache, aq.Kv8Batch(_i32(s.lens), _i32(s.table), _i32([0, 2] * ((n + 1) // 2))), q, out, scratch)
+    with pytest.raises(aq.AqError) as e:
+        aq.aq_check()
+    assert e.value.status == aq.AQ_ERR_RANGE and bool(torch.isnan(out).all())
+    marks = [0] * (n - 1) + [1, 2]
+    aq.aq_kv8_attn(s.cache, aq.Kv8Batch(_i32(s.lens), _i32(s.table), _i32(marks)), q, out, scratch)
+    aq.aq_check()
+    want, tol = _attn_reference(s, q.double().cpu().numpy(), [0] * (n - 2) + [1, 1], 0.0)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want))
+
+
+@pytest.mark.parametrize("D", (64, 256))
+def test_attention_tiny_queries_and_huge_keys(aq, D):
+    """bfloat16 rows under 2^-113 are in steps of 1 / 3e38.  Beside the module's tolerance: a score is off by half of that per element, under
+    2^-128 scale sum_d |K_d|, and by 2^-19 of itself more, as the step's product with the scale is a subnormal of 20 bits."""
+    s = Served(aq, [90], 1, D, 64, 18, spare=0)
+    up = 2.0 ** 114
+    s.ks = s.ks * up
+    s.cache = aq.Kv8Cache(s.k.cuda(), s.v.cuda(), s.ks.cuda(), s.vs.cuda())
+    q = (torch.randn(1, 6, D, generator=torch.Generator().manual_seed(18)) * 2.0 ** -116).to(torch.bfloat16)
+    out = torch.empty(1, 6, D, dtype=torch.float32, device="cuda")
+    aq.aq_kv8_attn(s.cache, s.batch(aq), q.cuda(), out, aq.aq_kv8_scratch())
+    aq.aq_check()
+    qh = q.double().numpy()
+    want, tol = _attn_reference(s, qh, [1], 0.0)
+    K, V = (O.gather(c.numpy(), sc.numpy(), s.table[0], 90) for c, sc in ((s.k, s.ks), (s.v, s.vs)))
+    for h in range(6):
+        _, T, _ = O.attn(qh[0, h], K[0], V[0], 1 / np.sqrt(D))
+        B = np.max(np.abs(K[0]) @ np.abs(qh[0, h])) / np.sqrt(D)
+        ds = 2.0 ** -128 * np.max(np.abs(K[0]).sum(1)) / np.sqrt(D) + 2.0 ** -19 * B
+        tol[0, h] += 3 * ds * T
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want))
+
+
 def test_attention_far_into_a_large_pool(aq):
     """Offsets past 2^32 bytes: pages at both ends of a pool of 4.6 GB of keys."""
     page, Hkv, D = 1024, 8, 256
