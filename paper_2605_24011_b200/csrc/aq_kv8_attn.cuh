@@ -34,9 +34,11 @@ namespace aq {
 constexpr int KA_TILE = AQ_KV8_BLOCK;                 // positions per tile: the span of a scale
 constexpr int KA_MAX_CTAS = 192;
 
-// QT: groups of four query rows.  A warp's ring has HALVES places; a place holds a tile's keys or its values, copied and waited for on their
-// own, and is filled again with what comes HALVES later when it has been used.  The first of a run's items may leave a piece: it takes
-// STEAL places, and the ring is that much shorter from then on.
+// QT: groups of four query rows.  A warp's ring has HALVES places; a place holds a tile's keys or its values and is filled again with what
+// comes HALVES later when it has been used: both when the tile is done where HALVES is even, so that its products and weights are one
+// stretch of code (ragged requests 70.1 -> 66.8 us), else the keys' before the weights, so that a half more is under way.
+// The first of a run's items may leave a piece.  It goes to one of POOL places beside the ring, by turns; when they are out it takes STEAL
+// places of the ring, which is that much shorter from then on (and that warp the CTA's last: without the POOL 66.8 us, with it 64.9).
 template <int D, int QT>
 struct KaShape {
     static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : D == 128 && QT <= 3 ? 12 : 8;
@@ -45,14 +47,18 @@ struct KaShape {
     static constexpr int HALF = KA_TILE * D;          // bytes of a tile's keys (or values)
     static constexpr int PITCH = D + 4;               // floats: a row's O, then its maximum and sum
     static constexpr int SLOT = ROWS * PITCH * 4;     // a piece
-    static constexpr int STEAL = QT <= 2 ? 1 : 2;
-    static constexpr int BUF = HALF + 16;             // a half, its scale and, with keys, whether the tile may be read
-    static constexpr int PLACE = BUF > SLOT / STEAL ? BUF : SLOT / STEAL;
+    static constexpr bool ONCE = HALVES % 2 == 0;     // a place is for keys or for values: a tile is waited for once
+    static constexpr int STEAL = ONCE ? 2 : 1;
+    // on a line of 128 bytes (with 16 more for the scale between places 32 x 4096 took 53.0 us, so 49.3)
+    static constexpr int PLACE = ((HALF > SLOT / STEAL ? HALF : SLOT / STEAL) + 127) / 128 * 128;
     static constexpr int RING = WARPS * HALVES * PLACE;
-    static constexpr int SMEM = RING + ROWS * 32 * 12;   // + for merging: a weight, a maximum and a sum per row and part
+    static constexpr int TAGS = WARPS * HALVES * 8;   // a place's scale and, with keys, whether the tile may be read
+    static constexpr int MERGE = ROWS * 32 * 12;      // a weight, a maximum and a sum per row and part
+    static constexpr int FITS = (232448 - 2600 - RING - TAGS - MERGE) / SLOT, POOL = FITS < WARPS ? FITS : WARPS;   // places for pieces beside the ring
+    static constexpr int SMEM = RING + MERGE + POOL * SLOT + TAGS;
     static_assert((AQ_KV8_MAX_SEQS + 1) * 4 <= RING && 14 * SLOT <= RING, "the line's marks, and the parts of a group, lie in the ring");
     static_assert(HALVES - STEAL >= 2 && (STEAL == 1 || HALVES % 2 == 0) && 2 * WARPS <= 32, "places can be spared; a lane per piece");
-    static_assert(SMEM + 2600 <= 232448 && PLACE % 16 == 0, "shared memory of an SM");
+    static_assert(SMEM + 2600 <= 232448 && SLOT % 16 == 0, "shared memory of an SM");
 };
 // scratch: tickets [2][KA_MAX_CTAS], parts [KA_MAX_CTAS][4][rows][pitch]
 constexpr size_t KA_TICKET_BYTES = 2 * KA_MAX_CTAS * 4;
@@ -113,6 +119,15 @@ __device__ __forceinline__ float ka_exp2(float x) {   // 2 ulp; results below 2^
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// o = f x + o and o = f o, two at a time
+__device__ __forceinline__ void ka_fma2(float (&o)[2], float x0, float x1, float f) {
+    asm("{.reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n mov.b64 c, {%0, %1};\n fma.rn.f32x2 c, a, b, c;\n mov.b64 {%0, %1}, c;}"
+        : "+f"(o[0]), "+f"(o[1]) : "f"(x0), "f"(x1), "f"(f));
+}
+__device__ __forceinline__ void ka_mul2(float (&o)[2], float f) {
+    asm("{.reg .b64 b, c;\n mov.b64 b, {%2, %2};\n mov.b64 c, {%0, %1};\n mul.rn.f32x2 c, c, b;\n mov.b64 {%0, %1}, c;}"
+        : "+f"(o[0]), "+f"(o[1]) : "f"(f));
 }
 // Byte offset of 16-byte piece c of row r in a tile: rows of eight that ldmatrix reads together fall on different banks.
 template <int D>
@@ -188,10 +203,15 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     __shared__ int last_flag[2], group_head[32];
     __shared__ KaSeq seqs[2 * W];   // the requests that a warp's copies and its products are at (kept out of the registers)
     __shared__ KaPiece at_work[W];
+    __shared__ int pool_used;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, t = lane & 3;
 
     // ---- the line: first place of each request ---------------------------------------------------------------
+    if constexpr (S::POOL < W) {
+        if (threadIdx.x == 0) pool_used = 0;
+        __syncthreads();
+    }
     pdl_wait();
     pdl_launch_dependents();
     if (lane < 2) pieces[2 * warp + lane].nt = 0;
@@ -326,6 +346,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     }
 
     const uint32_t my_ring = (uint32_t)(warp * S::HALVES * S::PLACE), ring = (uint32_t)__cvta_generic_to_shared(smem) + my_ring;
+    const uint32_t tags = (uint32_t)__cvta_generic_to_shared(smem) + S::SMEM - S::TAGS + warp * S::HALVES * 8;
 
     if (x0 < x1) {
         // ---- copies: a walk of its own, HALVES halves ahead --------------------------------------------------
@@ -383,19 +404,20 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         if constexpr (EARLY) load_queries(cs, item, 0);       // (under way while the first tiles' pages are looked up)
         bool p_ok = false;
         int64_t p_blk = 0;
-        auto copy = [&](uint32_t dst, const uint8_t* codes, const float* scales) {   // a tile's keys or values, and their scale
+        auto copy = [&](uint32_t dst, uint32_t tag, const uint8_t* codes, const float* scales) {   // a tile's keys or values, and their scale
             const uint8_t* src = codes + p_blk * S::HALF + lane * 16;
             // (the rows' pattern repeats every eight: a few offsets of the lane, the rest is known when this is compiled)
             constexpr int RPP = 512 / D, REP = RPP >= 8 ? 1 : 8 / RPP;
 #pragma unroll
             for (int i = 0; i < S::HALF / 512; ++i)
                 ka_cp16(dst + ka_at<D>(lane / (D / 16) + i % REP * RPP, lane % (D / 16)) + i / REP * (REP * 512), src + i * 512);
-            if (lane == 0) ka_cp4(dst + S::HALF, scales + p_blk);
+            if (lane == 0) ka_cp4(tag, scales + p_blk);
         };
         bool p_values = false;   // what is due: a tile's keys, or the values of the tile whose keys came last
-        auto issue = [&](int st) {
-            const uint32_t dst = ring + (uint32_t)(st * S::PLACE);
-            if (!p_values) {
+        auto issue = [&](int st, bool values) {
+            if (values && !p_values) return;   // (the run has no more tiles)
+            const uint32_t dst = ring + (uint32_t)(st * S::PLACE), tag = tags + (uint32_t)(st * 8);
+            if (!values) {
                 if (p_x >= x1) return;
                 const int pg = p_j >> a.shift;
                 if (p_page0 < 0 || pg >= p_page0 + 32 || pg < p_page0) {
@@ -408,10 +430,10 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 const int hk = ps.rb == 1 ? p_item : p_item / ps.rb;
                 p_blk = (((int64_t)page * a.Hkv + hk) << a.shift) + (p_j & ((1 << a.shift) - 1));
                 if (!p_ok && ps.L > 0 && lane == 0) kv8_report(KV8_BAD_PAGE);
-                if (lane == 1) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + S::HALF + 4), "r"(p_ok ? 1 : 0) : "memory");
+                if (lane == 1) asm volatile("st.shared.u32 [%0], %1;" ::"r"(tag + 4), "r"(p_ok ? 1 : 0) : "memory");
             }
-            if (p_ok) copy(dst, p_values ? a.vc : a.kc, p_values ? a.vs : a.ks);
-            if (p_values) {
+            if (p_ok) copy(dst, tag, values ? a.vc : a.kc, values ? a.vs : a.ks);
+            if (values) {
                 ++p_x;
                 if (++p_j == ps.nt) {
                     p_x += KV8_ITEM_COST;
@@ -422,11 +444,11 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     }
                 }
             }
-            p_values = !p_values;
+            p_values = !values;
         };
 #pragma unroll 1
         for (int s = 0; s < S::HALVES; ++s) {
-            issue(s);
+            issue(s, S::ONCE ? (s & 1) != 0 : p_values);
             ka_commit();
         }
 
@@ -517,14 +539,15 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             const bool item_ends = j + 1 == nt;
             const uint32_t next = x + 1 + (item_ends ? KV8_ITEM_COST : 0u);
             const bool run_ends = next >= x1, whole = item_ends && first >= x0, take = item_ends && !run_ends && !whole;
-            if (gone < 0) ka_wait<S::HALVES - 1>(); else ka_wait<S::HALVES - 1 - S::STEAL>();
+            constexpr int USED = S::ONCE ? 2 : 1;
+            if (gone < 0) ka_wait<S::HALVES - USED>(); else ka_wait<S::HALVES - USED - S::STEAL>();
             __syncwarp();   // every lane's copies of the keys have landed
             const int vst = after(kst);
             const uint32_t kt = ring + (uint32_t)(kst * S::PLACE), vt = ring + (uint32_t)(vst * S::PLACE);
             float ks;
             int ok;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(kt + S::HALF) : "memory");
-            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(ok) : "r"(kt + S::HALF + 4) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(tags + (uint32_t)(kst * 8)) : "memory");
+            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(ok) : "r"(tags + (uint32_t)(kst * 8) + 4) : "memory");
             // (ok is the same for all lanes; a tile that could not be read counts as masked)
             int sc[QT][2][4];
             if (ok) {
@@ -544,59 +567,73 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     }
                 }
             }
-            __syncwarp();   // every lane is through with the keys
-            if (take && S::STEAL == 2) {
-                ka_wait<S::HALVES - 2>();
-            } else {
-                issue(kst);
+            if constexpr (!S::ONCE) {
+                __syncwarp();   // every lane is through with the keys
+                issue(kst, p_values);
                 ka_commit();
                 if (gone < 0) ka_wait<S::HALVES - 1>(); else ka_wait<S::HALVES - 1 - S::STEAL>();
+                __syncwarp();   // every lane's copies of the values have landed
             }
-            __syncwarp();   // every lane's copies of the values have landed
             if (ok) {
                 float vs;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(vt + S::HALF) : "memory");
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(tags + (uint32_t)(vst * 8)) : "memory");
                 // ---- weights
                 const int pos = j * KA_TILE;
                 const bool all_seen = pos + KA_TILE <= lim_min;
+                // (Step by step over all groups, each step in one block of code: with the masks' branches inside a loop over groups the warp waited
+                // for one group after the other.)
                 uint32_t pb[QT][2];
                 float al[QT], vf[QT];
+                int s[QT][4], top[QT];   // positions g, g + 8, g + 16, g + 24 of row t
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[u][i] = sc[u][i >> 1][2 * (i & 1)] * 256 + sc[u][i >> 1][2 * (i & 1) + 1];
+                constexpr int NONE = -0x7fffffff - 1;   // (no score is so low: |S| <= 256 * 128 * 32639)
+                if (!all_seen) {
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[u][i] = pos + 8 * i + g < lim[u] ? s[u][i] : NONE;
+                }
+#pragma unroll
+                for (int u = 0; u < QT; ++u) top[u] = max(max(s[u][0], s[u][1]), max(s[u][2], s[u][3]));
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1)
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], d));
+                uint32_t p[QT][4];   // the low half: rint(65535 weight)
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    const float F = ks * fq[u];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float w = ka_exp2((float)(int)((uint32_t)s[u][i] - (uint32_t)top[u]) * F);
+                        p[u][i] = __float_as_uint(fmaf(w, 65535.f, 8388608.f));
+                    }
+                }
+                if (!all_seen) {
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[u][i] = s[u][i] == NONE ? 0u : p[u][i];
+                }
                 bool moved = false;
 #pragma unroll
                 for (int u = 0; u < QT; ++u) {
-                    int s[4];   // positions g, g + 8, g + 16, g + 24 of row t
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[i] = sc[u][i >> 1][2 * (i & 1)] * 256 + sc[u][i >> 1][2 * (i & 1) + 1];
-                    constexpr int NONE = -0x7fffffff - 1;   // (no score is so low: |S| <= 256 * 127 * (256 * 127 + 127))
-                    if (!all_seen) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) s[i] = pos + 8 * i + g < lim[u] ? s[i] : NONE;
-                    }
-                    int top = max(max(s[0], s[1]), max(s[2], s[3]));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float F = ks * fq[u];
-                    uint32_t p[4];   // the low half: rint(65535 weight)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float w = ka_exp2((float)(int)((uint32_t)s[i] - (uint32_t)top) * F);
-                        p[i] = __float_as_uint(fmaf(w, 65535.f, 8388608.f));
-                        if (!all_seen && s[i] == NONE) p[i] = 0u;
-                    }
                     int lt[4] = {0, 0, 0, 0};
                     const uint32_t ones[4] = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         // columns 2t, 2t + 1: row t's positions g and g + 8; transposed, lane (g, t) has two of the four positions 2t, 2t + 1, 2t + 8,
                         // 2t + 9 of row g / 2 and its neighbour the other two: even g takes the four high bytes, odd g the low ones
-                        const uint32_t mine = ka_transpose(__byte_perm(p[2 * h], p[2 * h + 1], 0x5410));
+                        const uint32_t mine = ka_transpose(__byte_perm(p[u][2 * h], p[u][2 * h + 1], 0x5410));
                         const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 4);
                         pb[u][h] = __byte_perm(mine, other, (g & 1) ? 0x2064 : 0x7531);
                     }
                     ka_mma_su(lt, ones, pb[u][0], pb[u][1]);
-                    const bool any = top != NONE;
-                    const float s_top = any ? (float)top * F : -INFINITY;
+                    const bool any = top[u] != NONE;
+                    const float s_top = any ? (float)top[u] * (ks * fq[u]) : -INFINITY;
                     const float now = fmaxf(m[u], s_top);   // (a NaN leaves the maximum; fac carries it into the sums)
                     al[u] = now == -INFINITY ? 1.f : ka_exp2(m[u] - now);
                     const float fac = any ? ka_exp2(s_top - (now == -INFINITY ? 0.f : now)) : 0.f;
@@ -610,7 +647,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
 #pragma unroll
                     for (int u = 0; u < QT; ++u)
 #pragma unroll
-                        for (int c = 0; c < D / 16; ++c) { o[u][c][0] *= al[u]; o[u][c][1] *= al[u]; }
+                        for (int c = 0; c < D / 16; ++c) ka_mul2(o[u][c], al[u]);
                 }
                 // ---- O += vs fac V P
 #pragma unroll
@@ -624,14 +661,28 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                     for (int u = 0; u < QT; ++u) {
                         int ot[4] = {0, 0, 0, 0};
                         ka_mma_su(ot, v, pb[u][0], pb[u][1]);
-                        o[u][c][0] = fmaf(vf[u], (float)(ot[0] * 256 + ot[1]), o[u][c][0]);
-                        o[u][c][1] = fmaf(vf[u], (float)(ot[2] * 256 + ot[3]), o[u][c][1]);
+                        ka_fma2(o[u][c], (float)(ot[0] * 256 + ot[1]), (float)(ot[2] * 256 + ot[3]), vf[u]);
                     }
                 }
             }
             __syncwarp();   // every lane is through with the values
-            if (!take) {
-                issue(vst);
+            bool steal = false;
+            uint32_t piece_at = 0;
+            if (take) {   // a place for the piece: beside the ring, or else where this tile was
+                int k = warp;
+                if constexpr (S::POOL < W) {
+                    if (lane == 0) k = atomicAdd(&pool_used, 1);
+                    k = __shfl_sync(0xffffffffu, k, 0);
+                    steal = k >= S::POOL;
+                }
+                piece_at = (uint32_t)(S::RING + S::MERGE + k * S::SLOT);
+            }
+            if (S::ONCE && !(steal && S::STEAL == 2)) {
+                issue(kst, false);
+                ka_commit();
+            }
+            if (!steal) {
+                issue(vst, S::ONCE ? true : p_values);
                 ka_commit();
             }
 
@@ -655,7 +706,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                 } else {
                     // the run's first piece, where this tile was, or its last: all copies have been used by then
                     const int to = S::STEAL == 1 ? vst : kst;   // (places of one tile lie side by side where two are wanted)
-                    pc.at = my_ring + (uint32_t)(to * S::PLACE);
+                    pc.at = take && !steal ? piece_at : my_ring + (uint32_t)(to * S::PLACE);
 #pragma unroll
                     for (int u = 0; u < QT; ++u) {
                         float* row = reinterpret_cast<float*>(smem + pc.at) + (4 * u + t) * S::PITCH;
@@ -664,7 +715,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
                         if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(m[u], l[u]);
                     }
                     if (lane == 0) pieces[2 * warp + (run_ends ? 1 : 0)] = pc;
-                    if (take) gone = to;
+                    if (steal) gone = to;
                 }
             }
             kst = after(vst);
