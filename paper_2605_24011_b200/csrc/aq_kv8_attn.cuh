@@ -42,7 +42,7 @@ constexpr int KA_MAX_CTAS = 192;
 template <int D, int QT>
 struct KaShape {
     static constexpr int WARPS = D == 64 ? (QT <= 2 ? 16 : 12) : D == 128 && QT <= 3 ? 12 : 8;
-    static constexpr int HALVES = D == 256 ? 3 : D == 128 && QT <= 3 ? 4 : 6;
+    static constexpr int HALVES = D == 256 ? 3 : D == 64 || QT <= 3 ? 4 : 6;
     static constexpr int ROWS = 4 * QT;               // query rows of an item
     static constexpr int HALF = KA_TILE * D;          // bytes of a tile's keys (or values)
     static constexpr int PITCH = D + 4;               // floats: a row's O, then its maximum and sum
@@ -218,16 +218,16 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     uint32_t total, items, longest;   // of the line: places, items, tiles of the longest item
     KaSeq sq{};
     uint32_t off = 0;             // the run's first place in its request
-    uint32_t n_cta, c0 = 0, c1 = 0, x0 = 0, x1 = 0;   // the CTA's share, the warp's run
+    uint32_t c0 = 0, c1 = 0, x0 = 0, x1 = 0;   // the CTA's share, the warp's run
     Kv8Cut cut{};
     bool whole_items = false;     // every item belongs to the CTA whose share holds its first place
     auto my_run = [&] {
-        n_cta = kv8_ctas(total, items, W, gridDim.x);
-        if (blockIdx.x >= n_cta) return;
-        cut = kv8_cut(total, n_cta);
-        c0 = kv8_begin(cut, blockIdx.x);
-        c1 = kv8_begin(cut, blockIdx.x + 1);
-        whole_items = longest <= kv8_whole_items(cut, W);
+        const uint32_t n = kv8_ctas(total, items, W, gridDim.x);
+        const uint32_t each = n == gridDim.x ? kv8_alike(total, items, longest, n) : 0u;   // (fewer: there is a CTA per item, or a place per warp)
+        cut = each ? Kv8Cut{each * (longest + KV8_ITEM_COST), 0u} : kv8_cut(total, n);
+        c0 = min(kv8_begin(cut, blockIdx.x), total);
+        c1 = min(kv8_begin(cut, blockIdx.x + 1), total);
+        whole_items = each != 0u || longest <= kv8_whole_items(cut, W);
     };
     auto cut_warps = [&] {   // (the places in front of the first tile of a share that begins with an item are no warp's work)
         const uint32_t a0 = whole_items ? min(c0 + KV8_ITEM_COST, c1) : c0;
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             if (lane >= d) upto += v;
         }
         my_run();
-        if (blockIdx.x >= n_cta) return;
+        if (c0 >= total) return;
         if (whole_items) {
             auto snap = [&](uint32_t x) -> uint32_t {
                 const unsigned at = __ballot_sync(0xffffffffu, upto - mine <= x && x < upto);
@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             before += ka_places(a, ka_seq(a, b, ROWS));
         }
         my_run();
-        if (blockIdx.x >= n_cta) return;
+        if (c0 >= total) return;
         __syncthreads();
         if (whole_items) {
             auto snap = [&](uint32_t x) -> uint32_t {

@@ -336,6 +336,12 @@ def test_attention_many_requests_with_long_ones_among_them(aq):
     _check_attn(aq, lens, 2, 2, 128, 64, rows=[min(L, int(v)) for L, v in zip(lens, g.integers(0, 9, 60))], seed=16, outs=("f32",))
 
 
+@pytest.mark.parametrize("n,Hkv,L", ((25, 4, 1700), (38, 4, 1700), (19, 8, 1601), (75, 2, 1300), (100, 3, 1300)))
+def test_attention_items_that_are_alike(aq, n, Hkv, L):
+    """100, 152, 152, 150 and 300 items of one length: whole ones for every CTA where that keeps most of them busy, parts otherwise."""
+    _check_attn(aq, [L] * n, Hkv, 2, 64, 64, seed=n)
+
+
 def test_attention_more_rows_than_a_pass_takes(aq):
     _check_attn(aq, [5000, 40, 2200], 1, 4, 128, 128, rows=[40, 2, 1], seed=17, outs=("f32",))
     _check_attn(aq, [3000, 40], 2, 8, 256, 64, rows=[5, 3], seed=18, outs=("f32",))

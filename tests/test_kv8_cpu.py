@@ -302,3 +302,54 @@ def test_oracle_attention_and_gather():
     assert np.array_equal(x, y)
     y = O.rope_rows(x, [5, 7], f, "pairs", 2.0)
     assert np.allclose((y[..., :6] ** 2).sum(-1), 4 * (x[..., :6] ** 2).sum(-1)) and np.array_equal(y[..., 6:], x[..., 6:])
+
+
+ALIKE = textwrap.dedent(r"""
+    #include <cstdio>
+    #include <initializer_list>
+    #include "aq_kv8_runs.h"
+    using namespace aq;
+    #define CHECK(c) do { if (!(c)) { std::printf("FAIL line %d: %s\n", __LINE__, #c); return 1; } } while (0)
+    int main() {
+        for (uint32_t most : {1u, 3u, 132u, 148u})
+            for (uint32_t items = 1; items < 1200; ++items)
+                for (uint32_t longest : {1u, 16u, 128u, 5000u, 0x7fffffffu / items - 2u}) {
+                    const uint32_t len = longest + KV8_ITEM_COST;
+                    const uint64_t all = (uint64_t)len * items;
+                    if (all >= 0x80000000u) continue;
+                    const uint32_t total = (uint32_t)all, each = kv8_alike(total, items, longest, most);
+                    // not where items differ
+                    CHECK(kv8_alike(total - 1u, items, longest, most) == 0u && kv8_alike(total + 1u, items, longest, most) == 0u);
+                    const uint32_t least = (items + most - 1u) / most, ctas = (items + least - 1u) / least;
+                    CHECK(each == 0u || each == least);
+                    CHECK((each == 0u) == ((uint64_t)items * 3u < (uint64_t)least * most * 2u));
+                    if (each == 0u) continue;
+                    CHECK(ctas * 3u >= most * 2u);
+                    // shares begin and end with items, in 32 bits, and cover the line; whose share a place is in
+                    const Kv8Cut cut{each * len, 0u};
+                    CHECK((uint64_t)each * len * most <= 0xffffffffu && (uint64_t)ctas * each * len >= total);
+                    uint32_t end = 0;
+                    for (uint32_t i = 0; i < most; ++i) {
+                        uint32_t a = kv8_begin(cut, i), e = kv8_begin(cut, i + 1);
+                        a = a < total ? a : total; e = e < total ? e : total;
+                        CHECK(a == end && a % len == 0u && e % len == 0u && (a < e) == (i < ctas));
+                        if (a < e) CHECK(kv8_cta_of(cut, a) == i && kv8_cta_of(cut, e - 1u) == i);
+                        end = e;
+                    }
+                    CHECK(end == total);
+                }
+        std::printf("ok\n");
+        return 0;
+    }
+""")
+
+
+def test_items_that_are_alike(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text(ALIKE)
+    subprocess.run([gxx, "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", HDR, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout == "ok\n", r.stdout + r.stderr
