@@ -6,7 +6,7 @@
 // taken off exactly, the rest (half a turn at most, so an error of 2^-25 turns in binary32) into sincospif: far positions cost one
 // multiplication in binary64 and no argument reduction.  A CTA has consecutive (row, head) pairs, one wave of CTAs all of them; it forms
 // its rows' angles once for all of their heads, in shared memory, so laid out that neighbouring threads read neighbouring entries.
-// 4000 rows x 40 heads of 128, bfloat16: 16.9 us, 0.74 of the measured copy rate.  With more units per thread or fewer CTAs per SM it is
+// 4000 rows x 40 heads of 128, bfloat16: 15.1 us, 0.83 of the measured copy rate.  With more units per thread or fewer CTAs per SM it is
 // slower (4 units held while the angles are formed: 28.8 us): issue slots and threads, not bytes in flight, are what it runs out of.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -33,6 +33,7 @@ struct RrArgs {
 };
 constexpr int RR_THREADS = 256, RR_UNITS = 2;   // units per thread and turn
 constexpr int RR_SMEM = 40 * 1024, RR_CTAS = 5;   // per SM
+constexpr int RR_AHEAD = 32 * 1024;
 
 // N neighbouring elements as they lie in memory (N = 8: 16-byte aligned; N = 1), and as float32.
 template <typename T, int N>
@@ -109,6 +110,15 @@ __global__ void __launch_bounds__(RR_THREADS, RR_CTAS) rope_rows_kernel(const __
     TD* y0 = reinterpret_cast<TD*>(a.out) + (int64_t)row0 * a.out_row;
     pdl_wait();
     pdl_launch_dependents();
+    // a CTA with work for several turns asks for its first 32 KB while the angles are formed (4000 rows x 40 heads: 16.9 -> 15.1 us, 20000 rows
+    // 76.8 -> 75.8, with all of them on their way at once 81.0; with fewer turns the extra instructions cost more than they save)
+    if (n > 2 * RR_UNITS * RR_THREADS) {
+        for (int p = threadIdx.x; p < min(count, RR_AHEAD / (a.D * (int)sizeof(TS))); p += RR_THREADS) {
+            const int dr = (int)kv8_div((uint32_t)(base + p), a.heads_magic), h = base + p - dr * a.heads;
+            const TS* x = x0 + (int64_t)dr * a.x_row + h * a.D;
+            for (int k = 0; k < a.D; k += 128 / (int)sizeof(TS)) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + k));
+        }
+    }
     // pair e of unit u lies at e * turned + u: neighbouring threads read neighbouring entries
     constexpr int PPU = TWO ? N : N / 2;   // pairs per unit
     for (int i = threadIdx.x; i < n_rows * half; i += RR_THREADS) {

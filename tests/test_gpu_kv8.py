@@ -183,6 +183,13 @@ def test_rope_rows(aq, case, how):
     assert torch.equal(x, before[:, :H])
 
 
+@pytest.mark.parametrize("how,case", (("in place", (4000, 40, 8, 128, 128, "half", "parts", 8.0, 120000, "bf16", "bf16")),
+                                      ("out", (2500, 40, 0, 128, 64, "pairs", "none", 1.0, 4096, "f32", "f16")),
+                                      ("one element off", (1500, 9, 1, 81, 38, "pairs", "none", 1.0, 4096, "f16", "f16"))), ids=str)
+def test_rope_rows_with_several_turns_per_thread(aq, how, case):
+    test_rope_rows(aq, case, how)
+
+
 # ---- a cache in use ------------------------------------------------------------------------------------------------
 def _up11(x):
     return ((x.contiguous().view(torch.int32) + 0x1FFF) & ~0x1FFF).view(torch.float32)
