@@ -20,11 +20,12 @@
 // Every warp has a contiguous run of the line (aq_kv8_runs.h) and streams it through its own cp.async ring without waiting for another
 // warp; runs differ by one place at most whatever the requests' lengths are.  What a warp finishes alone it writes; pieces of an item are merged
 // over the warps of the CTA in shared memory, then over the CTAs in the scratch by the last CTA to arrive (counters; nobody waits), in two
-// levels above 14 CTAs.  All sums go in a fixed order.  Where items are short a CTA's share is moved to whole ones.
-// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 54.4 us, 4.9 TB/s, 0.75 of the copy rate (a third of the time is
-// the unequal speed of the SMs, the first trips and the merges); one request of 512 positions, 32 heads: 7.8 us; 100001 positions, 8 heads of 256 on
-// 1: 24.9 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows): 70 us for 296 MB, bound by issue slots.
-// Fewer warps are slower where the arithmetic counts (61 ragged requests: 76 us with 8), more do not fit the registers (168 each
+// levels above 14 CTAs.  All sums go in a fixed order.  Where items are short, or all alike, a CTA's share is of whole ones.
+// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 46.7 us, 5.75 TB/s, 0.88 of the copy rate (from the L2 instead of
+// HBM it takes 32.8: what remains is the start, the unequal speed of the SMs and the merge in the CTA); one request of 512 positions, 32 heads:
+// 7.2 us; 100001 positions, 8 heads of 256 on 1: 24.6 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows):
+// 63.5 us for 296 MB (57.9 from the L2: bound by the arithmetic, 840 instructions a tile at 46 % of the issue slots).
+// Fewer warps are slower where the arithmetic counts (61 ragged requests: 66.3 us with 8), more do not fit the registers (168 each
 // with 12: with the walks' state in them 148 us).
 // (Included by aq_kv8.cu alone, which has the status word and the host calls.)
 #pragma once

@@ -1,5 +1,5 @@
 // How the attention over the paged 8-bit cache is dealt to CTAs and warps, and which rows of a step belong to which request: the
-// index arithmetic of aq_kv8.cu and aq_kv8_attn.cu.  Plain C++ (host and device), so it can be unit-tested without a GPU.
+// index arithmetic of aq_kv8.cu and aq_kv8_attn.cuh.  Plain C++ (host and device), so it can be unit-tested without a GPU.
 //
 // The work is a line: requests in order, within a request its items (key/value head, block of query rows), of each item first
 // KV8_ITEM_COST places for what an item costs beside its tiles (queries in, output out), then its tiles of 32 positions.  The line is
