@@ -394,8 +394,10 @@ static cudaError_t launch_kw(KwArgs& a, cudaStream_t s) {
     if ((int64_t)a.T >= 4 * (int64_t)a.B) {
         a.chunk = 32;
         const int64_t blocks = (a.T + 31) / 32;
-        a.heads = 1;   // per CTA: as many as leave each SM several CTAs, so that one's look-ups serve them all
-        while (a.heads < 8 && blocks * 2 * ((a.Hkv + 2 * a.heads - 1) / (2 * a.heads)) >= KW_CTAS * sm_count()) a.heads *= 2;
+        // per CTA: as many as leave each SM several CTAs, so that one's look-ups serve them all, but four at most: with up to eight the last CTAs
+        // run alone (32 heads of 64, 4000 rows: 21.1 us, 15.5 so; 8 chunks of 500 rows of 32 heads of 128: 31.8 and 27.2; one of 4000: 21.4 and 21.5)
+        a.heads = 1;
+        while (a.heads < 4 && blocks * 2 * ((a.Hkv + 2 * a.heads - 1) / (2 * a.heads)) >= KW_CTAS * sm_count()) a.heads *= 2;
         return launch_pdl(kv8_append_kernel<D, BF16, 4>, dim3((unsigned)blocks, (unsigned)((a.Hkv + a.heads - 1) / a.heads), 2), dim3(KW_WARPS * 32), 0, s, a);
     }
     // a decode step's rows are a unit each: a CTA each while there are few
