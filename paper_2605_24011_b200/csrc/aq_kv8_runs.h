@@ -1,5 +1,5 @@
-// How the attention over the paged 8-bit cache is dealt to CTAs and warps, and which rows of a step belong to which request: the
-// index arithmetic of aq_kv8.cu and aq_kv8_attn.cuh.  Plain C++ (host and device), so it can be unit-tested without a GPU.
+// How the attention over the paged 8-bit cache is dealt to CTAs and warps, which rows of a step belong to which request, and how a
+// block's scale is rounded: the whole-number arithmetic of aq_kv8.cu and aq_kv8_attn.cuh.  Plain C++ (host and device), so it can be unit-tested without a GPU.
 //
 // The work is a line: requests in order, within a request its items (key/value head, block of query rows), of each item first
 // KV8_ITEM_COST places for what an item costs beside its tiles (queries in, output out), then its tiles of 32 positions.  The line is
@@ -88,6 +88,20 @@ AQ_HD int kv8_merge_group(int n) {
     int g = 4;
     while (g * g < n) ++g;
     return g;
+}
+
+// Of the pattern x of a binary32 number >= 0: the pattern of the next one of 11 significant bits not below it.  A normal number's 13 last
+// bits go; of a subnormal, whose pattern is the number itself in steps of 2^-149, what is behind its first 11 bits.
+AQ_HD uint32_t kv8_up11(uint32_t x) {
+#ifdef __CUDA_ARCH__
+    const int top = 31 - __clz((int)x);
+#else
+    int top = -1;
+    while (top < 31 && x >> (top + 1) != 0u) ++top;
+#endif
+    const int drop = top > 23 ? 13 : top > 10 ? top - 10 : 0;
+    const uint32_t low = (1u << drop) - 1u;
+    return (x + low) & ~low;
 }
 
 }  // namespace aq

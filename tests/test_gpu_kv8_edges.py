@@ -1,0 +1,42 @@
+"""The paged 8-bit cache at the edges of what its calls document: subnormal blocks, lengths past the table, values near the end of the
+type's range, steps whose row marks descend, ragged batches of few items.  Oracle and tolerances as in test_gpu_kv8.py."""
+import numpy as np
+import pytest
+
+from oracle import kv8_oracle as O
+from test_gpu_kv8 import Served, _attn_reference, _check_append, _check_attn, _i32, aq  # noqa: F401  (aq: the module's fixture)
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _bf16_patterns(below, seed):
+    """bfloat16 values of either sign whose magnitudes have patterns under `below`: 0x80 is 2^-126, 1 is 2^-133."""
+    def fill(x):
+        g = torch.Generator().manual_seed(seed)
+        m = torch.randint(0, below, x.shape, generator=g) + 0x8000 * torch.randint(0, 2, x.shape, generator=g)
+        x.copy_(torch.where(m >= 0x8000, m - 0x10000, m).to(torch.int16).view(torch.bfloat16))
+    return fill
+
+
+@pytest.mark.parametrize("below", (2, 3, 0x10, 0x80, 0x100, 0x180, 0x400))
+@pytest.mark.parametrize("D", (64, 128, 256))
+def test_append_of_subnormal_blocks_is_exact(aq, D, below):
+    """Blocks whose scale is a subnormal binary32: the definition's 11 significant bits, not a multiple of 2^-136."""
+    _check_append(aq, [40, 77, 5], [1, 60, 5], 2, D, 64, "bf16", 90 + D, values=_bf16_patterns(below, below))
+    _check_append(aq, [1, 33, 64], None, 3, D, 64, "bf16", 91 + D, values=_bf16_patterns(below, below + 1))
+
+
+@pytest.mark.parametrize("start", (2.0 ** -133, 2.0 ** -128, 2.0 ** -124))
+def test_append_position_by_position_in_subnormals(aq, start):
+    """Scales that grow by a quarter through the subnormal range, older codes put on them."""
+    s = Served(aq, [64], 1, 64, 64, 92)
+    k, ks, v, vs = s.k.numpy(), s.ks.numpy(), s.v.numpy(), s.vs.numpy()
+    g = np.random.default_rng(93)
+    for L in range(1, 65):
+        x = torch.from_numpy(g.standard_normal((1, 2, 1, 64)) * start * 1.15 ** (L % 32)).to(torch.bfloat16)
+        aq.aq_kv8_append(s.cache, aq.Kv8Batch(_i32([L]), _i32(s.table)), x[:, 0].cuda(), x[:, 1].cuda())
+        k, ks, v, vs = O.append(k, ks, v, vs, [L], [0, 1], s.table, x[:, 0].float().numpy(), x[:, 1].float().numpy())
+    aq.aq_check()
+    for got, w in zip((s.cache.k, s.cache.k_scale, s.cache.v, s.cache.v_scale), (k, ks, v, vs)):
+        assert np.array_equal(got.cpu().numpy(), w, equal_nan=w.dtype.kind == "f")
