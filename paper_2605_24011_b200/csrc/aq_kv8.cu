@@ -264,9 +264,10 @@ __device__ __forceinline__ void kw_store(const KwUnit<D, WPU>& u, int w, uint32_
     }
     if (poison) s = __uint_as_float(0x7fc00000u);
     // A scale under 2^-60 (bfloat16 only) has no reciprocal to work with: both sides of the quotient times 2^100 then.  s = 0 is a block of
-    // zeros; of a NaN the codes do not matter, they become 0.
+    // zeros; of a NaN the codes do not matter, they become 0, as do those of an infinite scale (a caller's; quotients by it).
     const float lift = s < 8.67361737988403547e-19f ? 1.2676506002282294e30f : 1.f;
-    const float fit = s > 0.f ? s * lift : 1.f, inv = poison ? 0.f : 1.f / fit;
+    const bool endless = s > 3.402823466e38f;
+    const float fit = s > 0.f && !endless ? s * lift : 1.f, inv = poison || endless ? 0.f : 1.f / fit;
     auto pair = [&](uint32_t u, uint32_t& a, uint32_t& b) {
         float e, f;
         if constexpr (BF16) { e = __uint_as_float(u << 16); f = __uint_as_float(u & 0xffff0000u); }

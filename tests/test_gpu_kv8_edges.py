@@ -40,3 +40,22 @@ def test_append_position_by_position_in_subnormals(aq, start):
     aq.aq_check()
     for got, w in zip((s.cache.k, s.cache.k_scale, s.cache.v, s.cache.v_scale), (k, ks, v, vs)):
         assert np.array_equal(got.cpu().numpy(), w, equal_nan=w.dtype.kind == "f")
+
+
+def test_append_to_a_block_whose_scale_is_infinite(aq):
+    """need <= s' then: the scale stays, code = rint(x / inf) = 0, the older codes stay."""
+    s = Served(aq, [50, 20], 2, 128, 64, 94)
+    s.ks.nan_to_num_(0.25, 0.25)
+    s.vs.nan_to_num_(0.25, 0.25)
+    s.ks[s.table[0][0]], s.vs[s.table[1][0]] = float("inf"), float("inf")
+    s.cache = aq.Kv8Cache(s.k.cuda(), s.v.cuda(), s.ks.cuda(), s.vs.cuda())
+    x = torch.randn(5, 2, 2, 128, generator=torch.Generator().manual_seed(94)).half()
+    xd = x.cuda()
+    for rows in ([3, 2], [1, 4]):
+        aq.aq_kv8_append(s.cache, s.batch(aq, rows), xd[:, 0], xd[:, 1])
+    aq.aq_check()
+    want = (s.k.numpy(), s.ks.numpy(), s.v.numpy(), s.vs.numpy())
+    for rows in ([0, 3, 5], [0, 1, 5]):
+        want = O.append(*want, [50, 20], rows, s.table, x[:, 0].float().numpy(), x[:, 1].float().numpy())
+    for got, w in zip((s.cache.k, s.cache.k_scale, s.cache.v, s.cache.v_scale), want):
+        assert np.array_equal(got.cpu().numpy(), w, equal_nan=w.dtype.kind == "f")
