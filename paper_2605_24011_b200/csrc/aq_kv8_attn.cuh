@@ -139,7 +139,7 @@ __device__ __forceinline__ uint32_t ka_at(int r, int c) {
 
 // A request of the line.
 struct KaSeq {
-    int b, L, row0, n, nt, rb;   // nt: tiles of an item; rb: items per key/value head
+    int b, L, row0, n, nt, rb;   // L: as the caller says; nt: tiles of an item, those that the table has room for; rb: items per key/value head
 };
 __device__ __forceinline__ KaSeq ka_seq(const KaArgs& a, int b, int rows) {
     KaSeq s;
@@ -147,12 +147,15 @@ __device__ __forceinline__ KaSeq ka_seq(const KaArgs& a, int b, int rows) {
     const Kv8Rows r = a.row_start ? kv8_rows(a.row_start[b], a.row_start[b + 1], a.T) : Kv8Rows{b * a.n_each, a.n_each};
     s.row0 = r.first;
     s.n = r.n;
-    const int64_t most = a.width << (a.shift + 5);
-    s.L = (int)min((int64_t)max(a.lens[b], 0), most);
-    s.nt = max(1, (s.L + KA_TILE - 1) / KA_TILE);   // (a request without positions has one tile that is not read: its rows become 0)
+    s.L = max(a.lens[b], 0);   // (rows' positions follow from it, as the append has them, whether they fit or not)
+    const int held = (int)min((int64_t)s.L, a.width << (a.shift + 5));
+    s.nt = max(1, (held + KA_TILE - 1) / KA_TILE);   // (a request without positions has one tile that is not read: its rows become 0)
     s.rb = (s.n * a.G + rows - 1) / rows;   // (n G <= 2^20)
     return s;
 }
+
+// Whether a request has rows and a length that the table has no room for, or a negative one.
+__device__ __forceinline__ bool ka_too_long(const KaSeq& s, int len) { return s.n > 0 && (len < 0 || s.L > s.nt * KA_TILE); }
 
 __device__ __forceinline__ uint32_t ka_places(const KaArgs& a, const KaSeq& s) {
     return ((uint32_t)s.nt + KV8_ITEM_COST) * (uint32_t)s.rb * (uint32_t)a.Hkv;
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         KaSeq s{};
         if (lane < a.B) {
             s = ka_seq(a, lane, ROWS);
-            if (s.n > 0 && s.L != a.lens[lane]) kv8_report(KV8_BAD_LENGTH);
+            if (ka_too_long(s, a.lens[lane])) kv8_report(KV8_BAD_LENGTH);
         }
         const uint32_t mine = ka_places(a, s);
         total = __reduce_add_sync(0xffffffffu, mine);
@@ -287,7 +290,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             const KaSeq s = ka_seq(a, b, ROWS);
             if (s.n > 0) my_longest = max(my_longest, (uint32_t)s.nt);
-            if (s.n > 0 && s.L != a.lens[b]) kv8_report(KV8_BAD_LENGTH);
+            if (ka_too_long(s, a.lens[b])) kv8_report(KV8_BAD_LENGTH);
             mine += ka_places(a, s);
             my_rows += (uint32_t)s.n;
             my_items += (uint32_t)s.rb * (uint32_t)a.Hkv;

@@ -59,3 +59,31 @@ def test_append_to_a_block_whose_scale_is_infinite(aq):
         want = O.append(*want, [50, 20], rows, s.table, x[:, 0].float().numpy(), x[:, 1].float().numpy())
     for got, w in zip((s.cache.k, s.cache.k_scale, s.cache.v, s.cache.v_scale), want):
         assert np.array_equal(got.cpu().numpy(), w, equal_nan=w.dtype.kind == "f")
+
+
+@pytest.mark.parametrize("others", (1, 40))
+@pytest.mark.parametrize("D,rows", ((128, 8), (64, 3), (256, 17)))
+def test_attention_of_a_length_past_the_table(aq, D, rows, others):
+    """Only the positions that do not fit count as masked: a row's own position is where the caller's length puts it, as the append has it."""
+    page, width = 32, 3
+    s = Served(aq, [page * width] + [20] * others, 2, D, page, 95)
+    T = rows + others
+    q = torch.randn(T, 4, D, generator=torch.Generator().manual_seed(95)).half()
+    for past in (1, 5, 40, 2 ** 31 - 1 - page * width):
+        out = torch.full((T, 4, D), float("nan"), device="cuda")
+        batch = aq.Kv8Batch(_i32([page * width + past] + [20] * others), _i32(s.table), _i32([0] + list(range(rows, T + 1))))
+        aq.aq_kv8_attn(s.cache, batch, q.cuda(), out, aq.aq_kv8_scratch())
+        with pytest.raises(aq.AqError) as e:
+            aq.aq_check()
+        assert e.value.status == aq.AQ_ERR_RANGE
+        got = out.double().cpu().numpy()
+        for i in range(rows):
+            # the row as the only new token of a request of the length that it sees
+            one = Served.__new__(Served)
+            one.k, one.ks, one.v, one.vs, one.table, one.Hkv = s.k, s.ks, s.v, s.vs, s.table, 2
+            one.lens = [min(page * width, page * width + past - rows + i + 1)]
+            want, tol = _attn_reference(one, q[i: i + 1].double().numpy(), [1], 0.0)
+            assert np.all(np.abs(got[i] - want[0]) <= tol[0] * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want[0])), (past, i)
+        s.lens = [0] + [20] * others
+        want, tol = _attn_reference(s, q.double().numpy()[rows:], [0] + [1] * others, 0.0)
+        assert np.all(np.abs(got[rows:] - want) <= tol * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want))
