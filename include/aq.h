@@ -270,7 +270,8 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
  * 2^-16 of it at most; bfloat16 rows under 2^-113: by 2^-128), the products with the codes are exact, weights enter the second product in 16 bits against the largest of their 32
  * positions (off by 2^-17 of that) and are summed as rounded, sums over positions are binary32: against the exact result for the
  * cached values an output is off by at most about 2^-12 (sum_p softmax_p |V[p]| + what that sum would be with every |V[p]| at its block's
- * largest), the scores' part and its own rounding.  A query row with a NaN or an infinity gives NaN.
+ * largest), the scores' part and its own rounding.  bfloat16 values: the sum of their magnitudes over the positions has to fit binary32, and the absolute
+ * error grows by 2^-122 for every 32 positions.  A query row with a NaN or an infinity gives NaN.
  * Sums go in a fixed order: the same call gives the same bits.
  * Errors of the aq_kv8 calls: AQ_ERR_INVALID_ARG (null / misaligned pointer, a size outside the ranges above, a stride that is no multiple of 8 or
  * shorter than a row, a scratch that is too small), AQ_ERR_UNSUPPORTED (head_dim, dtype, more than 256 key/value heads, more than 256 query heads for

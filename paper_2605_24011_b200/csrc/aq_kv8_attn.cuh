@@ -15,7 +15,7 @@
 //   P = rint(65535 exp2(S - the tile's largest S)): 16 bits against the tile's own largest weight, so a tile loses what lies under
 //       2^-17 of that and no tile is lost for being light.  Transposed by movmatrix and split into byte planes by a permute.  sum(P) is a
 //       product with ones: the normaliser sums what the values are weighted with.
-//   O = al O + vs fac (256 hi + lo) in binary32; ldmatrix.trans on pairs of bytes gives dims 2g, 2g + 1 of two positions per register.
+//   O = al O + 2^-16 vs fac (256 hi + lo) in binary32 (2^-16: the sum of weighted values fits where the values' own sum does); ldmatrix.trans on pairs of bytes gives dims 2g, 2g + 1 of two positions per register.
 // A NaN (of a scale, of a query row) travels in the scales: F, fac.
 // Every warp has a contiguous run of the line (aq_kv8_runs.h) and streams it through its own cp.async ring without waiting for another
 // warp; runs differ by one place at most whatever the requests' lengths are.  What a warp finishes alone it writes; pieces of an item are merged
@@ -184,8 +184,8 @@ __device__ __forceinline__ int64_t ka_out_at(const KaArgs& a, int row0, int hk, 
     const int tok = (int)kv8_div((uint32_t)q, a.G_magic);
     return (int64_t)(row0 + tok) * a.out_row + (int64_t)(hk * a.G + (q - tok * a.G)) * D;
 }
-// one over the normaliser; a row that saw nothing is 0
-__device__ __forceinline__ float ka_norm(float l) { return l == 0.f ? 0.f : 1.f / l; }
+// 2^16 over the normaliser (O was summed with 2^-16); a row that saw nothing is 0
+__device__ __forceinline__ float ka_norm(float l) { return l == 0.f ? 0.f : 1.f / l * 65536.f; }
 
 // Arrives at an item's (or a group's) counter: whether this was the last of `want`, who puts it back to zero.  What the CTA wrote before
 // the barrier in front of this is visible to whoever arrives later, and what earlier ones wrote to this CTA after the next barrier.
@@ -581,6 +581,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             if (ok) {
                 float vs;
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(tags + (uint32_t)(vst * 8)) : "memory");
+                vs *= 0x1p-16f;
                 // ---- weights
                 const int pos = j * KA_TILE;
                 const bool all_seen = pos + KA_TILE <= lim_min;

@@ -87,3 +87,37 @@ def test_attention_of_a_length_past_the_table(aq, D, rows, others):
         s.lens = [0] + [20] * others
         want, tol = _attn_reference(s, q.double().numpy()[rows:], [0] + [1] * others, 0.0)
         assert np.all(np.abs(got[rows:] - want) <= tol * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want))
+
+
+@pytest.mark.parametrize("up,lens,D", ((2.0 ** 109, [700, 33], 128), (2.0 ** 112, [60, 1], 64), (2.0 ** 106, [9000], 256)))
+def test_attention_of_values_near_the_end_of_the_range(aq, up, lens, D):
+    """bfloat16 reaches 3.4e38: the weighted sum of the values stays in binary32 as long as the sum of the values does."""
+    s = Served(aq, lens, 2, D, 64, 96)
+    s.vs = s.vs * up
+    s.cache = aq.Kv8Cache(s.k.cuda(), s.v.cuda(), s.ks.cuda(), s.vs.cuda())
+    q = torch.randn(len(lens), 8, D, generator=torch.Generator().manual_seed(96)).to(torch.bfloat16)
+    want, tol = _attn_reference(s, q.double().numpy(), [1] * len(lens), 0.0)
+    assert np.max(np.abs(want)) * max(lens) < 2.0 ** 127
+    for name, half in ((torch.float32, 2.0 ** -24), (torch.bfloat16, 2.0 ** -8)):
+        out = torch.empty(len(lens), 8, D, dtype=name, device="cuda")
+        aq.aq_kv8_attn(s.cache, s.batch(aq), q.cuda(), out, aq.aq_kv8_scratch())
+        aq.aq_check()
+        got = out.double().cpu().numpy()
+        assert np.all(np.abs(got - want) <= tol + half * (np.abs(want) + tol))
+
+
+@pytest.mark.parametrize("down", (2.0 ** -90, 2.0 ** -110, 2.0 ** -140))
+def test_attention_of_tiny_values(aq, down):
+    """Beside the module's tolerance 2^-122 per tile of 32 positions: a tile's scale enters as vs 2^-16 times its weight, off by 2^-150 at most where
+    that is subnormal, and is multiplied by 128 (65535 w) at most for each position, over the normaliser, 65535 2^-16 at least; the binary32
+    sums and the quotient are off by 2^-150 each there."""
+    s = Served(aq, [100, 1], 2, 128, 64, 97)
+    s.vs = (s.vs.double() * down).float()
+    s.cache = aq.Kv8Cache(s.k.cuda(), s.v.cuda(), s.ks.cuda(), s.vs.cuda())
+    q = torch.randn(2, 8, 128, generator=torch.Generator().manual_seed(97)).to(torch.bfloat16)
+    want, tol = _attn_reference(s, q.double().numpy(), [1, 1], 0.0)
+    out = torch.empty(2, 8, 128, device="cuda")
+    aq.aq_kv8_attn(s.cache, s.batch(aq), q.cuda(), out, aq.aq_kv8_scratch())
+    aq.aq_check()
+    # (the reference's tolerance has 1e-30 of its own, far more than these values: it goes)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= (tol - 1e-30) * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want) + 4 * 2.0 ** -122)
