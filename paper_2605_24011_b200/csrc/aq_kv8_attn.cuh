@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         x1 = kv8_warp_begin(a0, c1, warp + 1, W);
     };
     // Row marks that descend can name more rows than the step has, and the line would be longer than the host could know (it counts in 32
-    // bits): such a step is not followed.
+    // bits, and `total` may be anything, 0 too): such a step is not followed.
     auto too_many = [&](uint32_t rows) {
         if (rows <= (uint32_t)a.T) return false;
         if (blockIdx.x == 0 && threadIdx.x == 0) kv8_report(KV8_BAD_LENGTH);
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
         total = __reduce_add_sync(0xffffffffu, mine);
         items = __reduce_add_sync(0xffffffffu, (unsigned)(s.rb * a.Hkv));
         longest = __reduce_max_sync(0xffffffffu, s.n > 0 ? (unsigned)s.nt : 0u);
-        if (total == 0 || too_many(__reduce_add_sync(0xffffffffu, (unsigned)s.n))) return;
+        if (too_many(__reduce_add_sync(0xffffffffu, (unsigned)s.n)) || total == 0) return;
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
             longest = max(longest, sums[w][2]);
             rows += sums[w][3];
         }
-        if (total == 0 || too_many(rows)) return;
+        if (too_many(rows) || total == 0) return;
         for (int b = b0; b < min(b0 + per, a.B); ++b) {
             marks[b] = before;
             before += ka_places(a, ka_seq(a, b, ROWS));

@@ -121,3 +121,16 @@ def test_attention_of_tiny_values(aq, down):
     aq.aq_check()
     # (the reference's tolerance has 1e-30 of its own, far more than these values: it goes)
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= (tol - 1e-30) * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(want) + 4 * 2.0 ** -122)
+
+
+def test_attention_row_marks_whose_line_wraps(aq):
+    """Descending marks of 1024 requests that name 2^21 rows: a line of 2^32 places, 0 in 32 bits, is reported like any other."""
+    n, L = 1024, 8190 * 32
+    cache = aq.Kv8Cache(*(torch.zeros(2, 1, 1024, 64, dtype=torch.int8, device="cuda") for _ in range(2)), *(torch.ones(2, 1, 32, device="cuda") for _ in range(2)))
+    batch = aq.Kv8Batch(_i32([L] * n), _i32(np.zeros((n, 256))), _i32([0, 4096] * (n // 2) + [0]))
+    q = torch.zeros(4096, 4, 64, dtype=torch.float16, device="cuda")
+    out = torch.full((4096, 4, 64), float("nan"), dtype=torch.float16, device="cuda")
+    aq.aq_kv8_attn(cache, batch, q, out, aq.aq_kv8_scratch())
+    with pytest.raises(aq.AqError) as e:
+        aq.aq_check()
+    assert e.value.status == aq.AQ_ERR_RANGE and bool(torch.isnan(out).all())
