@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(KaShape<D, QT>::WARPS * 32, 1) kv8_attn_kernel
     Kv8Cut cut{};
     bool whole_items = false;     // every item belongs to the CTA whose share holds its first place
     auto my_run = [&] {
-        const uint32_t n = kv8_ctas(total, items, W, gridDim.x);
+        const uint32_t n = kv8_launch(total, items, longest, W, gridDim.x);
         const uint32_t each = n == gridDim.x ? kv8_alike(total, items, longest, n) : 0u;   // (fewer: there is a CTA per item, or a place per warp)
         cut = each ? Kv8Cut{each * (longest + KV8_ITEM_COST), 0u} : kv8_cut(total, n);
         c0 = min(kv8_begin(cut, blockIdx.x), total);

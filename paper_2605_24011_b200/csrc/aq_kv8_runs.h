@@ -17,13 +17,16 @@ namespace aq {
 
 constexpr uint32_t KV8_ITEM_COST = 2;
 
-// CTAs of a launch over a line of `total` places with `items` items, `warps` warps each, at most `most`.  Where there is a CTA for
-// every item and its warps have few tiles of it (five places), one each: nothing is then merged between CTAs, which costs a chain
-// of trips to memory (32 items of 16 tiles: 12.2 us with two CTAs per item).  Else a place per warp at least.
-AQ_HD uint32_t kv8_ctas(uint32_t total, uint32_t items, uint32_t warps, uint32_t most) {
-    if (items <= most && total <= items * warps * 5u) return items;
+// CTAs of a launch over a line of `total` places, `warps` warps each, at most `most`: so many that a warp has about a place.
+AQ_HD uint32_t kv8_even_ctas(uint32_t total, uint32_t warps, uint32_t most) {
     const uint32_t n = (total + warps - 1u) / warps;
     return n < most ? n : most;
+}
+// The same over `items` items that may be one CTA's each.  Where there is a CTA for every item and its warps have few tiles of it on average
+// (five places), one each: nothing is then merged between CTAs, which costs a chain of trips to memory (32 items of 16 tiles: 12.2 us with two
+// CTAs per item).
+AQ_HD uint32_t kv8_ctas(uint32_t total, uint32_t items, uint32_t warps, uint32_t most) {
+    return items <= most && total <= items * warps * 5u ? items : kv8_even_ctas(total, warps, most);
 }
 
 // How a line of `total` places is cut into `n` CTAs' shares (1 <= n <= total): the first `more` have one place more than the others.  One
@@ -43,6 +46,16 @@ AQ_HD uint32_t kv8_cta_of(const Kv8Cut& c, uint32_t x) {
 AQ_HD uint32_t kv8_whole_items(const Kv8Cut& c, uint32_t warps) {
     const uint32_t few = 4u * warps, part = c.each / 16u;
     return few > part ? few : part;
+}
+// Whether items, the longest of so many tiles, are one CTA's each where kv8_ctas says a CTA per item: all are short (kv8_whole_items of a cut
+// into `items` shares) or all alike (the cut then falls between them).
+AQ_HD bool kv8_stay_whole(uint32_t total, uint32_t items, uint32_t longest, uint32_t warps) {
+    return longest <= 4u * warps || (uint64_t)(longest + KV8_ITEM_COST) * items == total;
+}
+// CTAs of a launch, whatever the items are.  A long item among short ones, which the average hides, would be shared by CTAs all the same, and
+// few of them would run (items of 600 and 39 x 29 tiles: 14.3 us on 40 CTAs, 13.5 so; 100 and 31 x 45: 13.5 and 9.3).
+AQ_HD uint32_t kv8_launch(uint32_t total, uint32_t items, uint32_t longest, uint32_t warps, uint32_t most) {
+    return kv8_stay_whole(total, items, longest, warps) ? kv8_ctas(total, items, warps, most) : kv8_even_ctas(total, warps, most);
 }
 // Items that are all alike, on two thirds of the CTAs at least: how many whole ones a CTA gets, for two thirds of the SMs draw the memory's
 // whole rate and nothing is then merged between CTAs (256 items of 128 tiles: 49.7 us on 148 CTAs, 46.2 on 128; 120 items: 28.4 and

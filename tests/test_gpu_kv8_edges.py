@@ -134,3 +134,10 @@ def test_attention_row_marks_whose_line_wraps(aq):
     with pytest.raises(aq.AqError) as e:
         aq.aq_check()
     assert e.value.status == aq.AQ_ERR_RANGE and bool(torch.isnan(out).all())
+
+
+@pytest.mark.parametrize("D,G", ((64, 1), (128, 4), (256, 8)))
+def test_attention_few_items_and_one_long_one(aq, D, G):
+    """Fewer items than CTAs, one far longer than the average: shared by CTAs while the others stay short."""
+    _check_attn(aq, [600 * 32] + [29 * 32] * 39, 1, G, D, 128, seed=98, outs=("f32",))
+    _check_attn(aq, [9, 60 * 32, 40, 64], 2, G, D, 32, rows=[1, 2, 1, 0], seed=99, outs=("f32",))

@@ -39,3 +39,37 @@ def test_up11_of_all_magnitudes(tmp_path):
         got, want = lib.up11(x), O.up11(np.uint32(x).view(np.float32))
         assert got == int(want.view(np.uint32)), hex(x)
     assert lib.up11(0x7F800000) == 0x7F800000
+
+
+def test_ctas_of_ragged_items(tmp_path):
+    """A CTA per item only where no item is then shared by CTAs; else a CTA for every so many places."""
+    exe = _compiled(tmp_path, "ctas", r"""
+        #include <cstdio>
+        #include <initializer_list>
+        #include "aq_kv8_runs.h"
+        using namespace aq;
+        #define CHECK(c) do { if (!(c)) { std::printf("FAIL line %d: %s\n", __LINE__, #c); return 1; } } while (0)
+        int main() {
+            for (uint32_t W : {8u, 12u, 16u})
+                for (uint32_t most : {1u, 20u, 148u})
+                    for (uint32_t items = 1; items <= 200; ++items)
+                        for (uint32_t rest : {1u, 2u, 10u, 29u, 50u, 70u})
+                            for (uint32_t longest : {1u, 2u, 29u, 4u * W, 4u * W + 1u, 60u, 100u, 600u, 100000u}) {
+                                if (longest < rest) continue;
+                                const uint32_t total = longest + KV8_ITEM_COST + (items - 1u) * (rest + KV8_ITEM_COST);
+                                const uint32_t n = kv8_launch(total, items, longest, W, most), even = kv8_even_ctas(total, W, most);
+                                CHECK(n >= 1u && n <= most && n <= total);
+                                const Kv8Cut cut = kv8_cut(total, n);
+                                const bool alike = cut.more == 0u && cut.each == longest + KV8_ITEM_COST;
+                                // fewer CTAs than the places ask for, or more: a CTA per item, and none of them shared
+                                if (n != even) CHECK(n == items && (longest <= kv8_whole_items(cut, W) || alike));
+                                // and as before where all are short or alike
+                                if (longest <= 4u * W || rest == longest) CHECK(n == kv8_ctas(total, items, W, most));
+                            }
+            CHECK(kv8_launch(602u + 39u * 31u, 40u, 600u, 12u, 148u) == 148u && kv8_launch(32u * 18u, 32u, 16u, 12u, 148u) == 32u);
+            std::printf("ok\n");
+            return 0;
+        }
+    """, "-fsanitize=undefined", "-fno-sanitize-recover")
+    r = subprocess.run([exe], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout == "ok\n", r.stdout + r.stderr
