@@ -366,7 +366,7 @@ def aq_kv8_append(cache: Kv8Cache, batch: Kv8Batch, k, v, stream=None):
 def aq_kv8_scratch(device=None):
     """Scratch for aq_kv8_attn, zeroed (CUDA uint8)."""
     import torch
-    return torch.zeros(AQ_KV8_SCRATCH_BYTES, dtype=torch.uint8, device=device or "cuda")
+    return torch.zeros(AQ_KV8_SCRATCH_BYTES, dtype=torch.uint8, device="cuda" if device is None else device)
 
 
 def aq_kv8_attn(cache: Kv8Cache, batch: Kv8Batch, q, out, scratch, scale: float = 0.0, stream=None):

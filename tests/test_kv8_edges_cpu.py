@@ -73,3 +73,14 @@ def test_ctas_of_ragged_items(tmp_path):
     """, "-fsanitize=undefined", "-fno-sanitize-recover")
     r = subprocess.run([exe], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout == "ok\n", r.stdout + r.stderr
+
+
+def test_scratch_is_on_the_device_that_was_named(monkeypatch):
+    """Device 0 by its number is not the current device."""
+    torch = pytest.importorskip("torch")
+    from paper_2605_24011_b200 import aq
+    asked = []
+    monkeypatch.setattr(torch, "zeros", lambda n, dtype, device: asked.append((n, dtype, device)))
+    for device in (0, 1, "cuda:0", torch.device("cuda", 0), None):
+        aq.aq_kv8_scratch() if device is None else aq.aq_kv8_scratch(device)
+    assert asked == [(aq.AQ_KV8_SCRATCH_BYTES, torch.uint8, d) for d in (0, 1, "cuda:0", torch.device("cuda", 0), "cuda")]
