@@ -3,6 +3,7 @@ import ctypes as C
 import os
 import shutil
 import subprocess
+import sys
 import textwrap
 
 import numpy as np
@@ -84,3 +85,46 @@ def test_scratch_is_on_the_device_that_was_named(monkeypatch):
     for device in (0, 1, "cuda:0", torch.device("cuda", 0), None):
         aq.aq_kv8_scratch() if device is None else aq.aq_kv8_scratch(device)
     assert asked == [(aq.AQ_KV8_SCRATCH_BYTES, torch.uint8, d) for d in (0, 1, "cuda:0", torch.device("cuda", 0), "cuda")]
+
+
+@pytest.fixture
+def builder(tmp_path, monkeypatch):
+    """The build with compilers that only write their outputs: (module, list of programs run, set of those that fail)."""
+    from paper_2605_24011_b200 import build as B
+    ran, failing = [], set()
+
+    def run(cmd, **kw):
+        ran.append(os.path.basename(cmd[0]))
+        bad = ran[-1] in failing
+        if not bad:
+            with open(cmd[cmd.index("-o") + 1], "w") as f:
+                f.write("x")
+        return subprocess.CompletedProcess(cmd, int(bad), "", "it failed" if bad else "")
+    monkeypatch.setattr(B, "subprocess", type("Fake", (), {"run": staticmethod(run)}))
+    monkeypatch.setattr(B, "OUT", str(tmp_path / "libaq.so"))
+    monkeypatch.setattr(B, "TORCH_OUT", str(tmp_path / "_aq_torch.so"))
+    monkeypatch.setattr(B, "OBJ", str(tmp_path / "_build"))
+    return B, ran, failing
+
+
+def test_library_is_built_without_torch(builder, monkeypatch, capsys):
+    B, ran, _ = builder
+    monkeypatch.setitem(sys.modules, "torch", None)   # an import fails
+    assert B.build() == B.OUT and os.path.exists(B.OUT) and not os.path.exists(B.TORCH_OUT)
+    assert "torch" in capsys.readouterr().err and "g++" not in ran
+    n = len(ran)
+    B.build()
+    assert len(ran) == n   # the library is not linked again for the sake of what cannot be built
+
+
+def test_library_is_there_when_the_calls_on_tensors_do_not_compile(builder):
+    pytest.importorskip("torch")
+    B, ran, failing = builder
+    failing.add("g++")
+    with pytest.raises(RuntimeError, match="aq_torch"):
+        B.build()
+    assert os.path.exists(B.OUT) and not os.path.exists(B.TORCH_OUT)
+    failing.clear()
+    ran.clear()
+    B.build()
+    assert ran == ["g++"] and os.path.exists(B.TORCH_OUT)
