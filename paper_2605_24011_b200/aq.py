@@ -294,13 +294,16 @@ class _Calls:
         import importlib.machinery
         import importlib.util
 
-        import torch  # noqa: F401  (the module needs its libraries loaded)
+        from .build import torch_key
+        key = torch_key()   # (which imports torch: the module needs its libraries loaded)
         path = os.path.join(_HERE, "_aq_torch.so")
         if not os.path.exists(path):
             raise ImportError(f"{path} not found: build it with `python -m paper_2605_24011_b200.build`")
         spec = importlib.util.spec_from_file_location("_aq_torch", path, loader=importlib.machinery.ExtensionFileLoader("_aq_torch", path))
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
+        if getattr(mod, "built_for", None) != key:
+            raise ImportError(f"{path} was not built for {key}: build it again with `python -m paper_2605_24011_b200.build`")
         mod.bind(*(C.cast(f, C.c_void_p).value for f in (_lib.aq_kv8_plan, _lib.aq_kv8_append, _lib.aq_kv8_attn, _lib.aq_rope_rows)))
         global _calls
         _calls = mod

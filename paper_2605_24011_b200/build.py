@@ -46,6 +46,12 @@ def _compile(src):
     return obj
 
 
+def torch_key() -> str:
+    """What a binary of _aq_torch.so belongs to: this interpreter and its torch."""
+    import torch
+    return f"torch {torch.__version__} cxx11abi {int(torch._C._GLIBCXX_USE_CXX11_ABI)} {sysconfig.get_config_var('SOABI')}"
+
+
 def _compile_torch(force: bool = False):
     """_aq_torch.so, against the torch that this interpreter has (its headers and libraries, no others).  Returns what is missing for it, or None."""
     include = sysconfig.get_paths()["include"]
@@ -57,19 +63,23 @@ def _compile_torch(force: bool = False):
         return "no g++"
     if not os.path.exists(os.path.join(include, "Python.h")):
         return f"no Python.h in {include}"
-    src = os.path.join(CSRC, "aq_torch.cpp")
+    src, key_file, key = os.path.join(CSRC, "aq_torch.cpp"), os.path.join(OBJ, "aq_torch.key"), torch_key()
     deps = max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "aq.h")))
-    if not force and os.path.exists(TORCH_OUT) and os.path.getmtime(TORCH_OUT) >= deps:
-        return None
+    if not force and os.path.exists(TORCH_OUT) and os.path.getmtime(TORCH_OUT) >= deps and os.path.exists(key_file):
+        with open(key_file) as f:
+            if f.read() == key:
+                return None
     root = os.path.dirname(torch.__file__)
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), include,
            os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")]
     lib = os.path.join(root, "lib")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DAQ_BUILT_FOR="{key}"',
            *(f"-I{i}" for i in inc), src, "-o", TORCH_OUT, f"-L{lib}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on aq_torch.cpp:\n{r.stdout}\n{r.stderr}")
+    with open(key_file, "w") as f:
+        f.write(key)
     return None
 
 

@@ -176,4 +176,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_aq_torch", nullptr, -1, methods, 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__aq_torch() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__aq_torch() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", AQ_BUILT_FOR) < 0) {   // the interpreter and the torch that it was compiled against
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

@@ -128,3 +128,25 @@ def test_library_is_there_when_the_calls_on_tensors_do_not_compile(builder):
     ran.clear()
     B.build()
     assert ran == ["g++"] and os.path.exists(B.TORCH_OUT)
+
+
+def test_calls_on_tensors_are_compiled_again_for_another_torch(builder, monkeypatch):
+    torch = pytest.importorskip("torch")
+    B, ran, _ = builder
+    B.build()
+    assert "g++" in ran
+    ran.clear()
+    B.build()
+    assert ran == []
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    B.build()
+    assert ran == ["g++"]
+
+
+def test_calls_on_tensors_for_another_torch_are_not_loaded(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from paper_2605_24011_b200 import aq
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    monkeypatch.setattr(aq, "_calls", aq._Calls())
+    with pytest.raises(ImportError, match="0.0.1"):
+        aq.aq_rope_rows(aq.aq_rope_setup(64), torch.zeros(1, 1, 64), torch.zeros(1, dtype=torch.int32))
