@@ -191,6 +191,8 @@ aq_status_t aq_attn_decode(const void* q_dev, const void* k_cache_dev, const voi
  * its length not read; 1 <= table_width <= 2^20, table_width * page <= 2^30).  The step's arrays have n_rows rows (1 .. AQ_MAX_M); rows
  * row_start_dev[b] .. row_start_dev[b + 1] - 1 are request b's new tokens, its last positions in order; rows from
  * row_start_dev[n_seqs] on are nobody's and left as they are.  row_start_dev NULL: n_rows / n_seqs rows each (n_rows % n_seqs == 0).
+ * Rows of nobody cost the kernels little, but n_rows chooses their form: many rows per request on average are taken for prompts.  A
+ * step that is recorded once with room for prompts runs that form for its decode steps too; record those apart, with fewer rows.
  * Two requests may share pages that neither writes to.  The descriptors are read during the call; the arrays they name are read by its stream
  * work, so a captured call follows new lengths, tables and rows.
  *
@@ -233,7 +235,9 @@ typedef struct {
  *                          request's pages in order; giving back comes first)
  *   lens_out_dev [n_seqs], n_free_out_dev : lengths and free pages after the step (0 for an ended request; may be lens_dev and n_free_dev)
  *   row_start_dev [n_seqs + 1], pos_dev [n_rows] : first row of each request, and of each row its position (-1: nobody's row)
- * page and table_width as above; 1 <= n_rows <= 2^20, 0 <= free_cap < 2^31.
+ * page and table_width as above; 1 <= n_rows <= 2^20 (a step for aq_kv8_append and aq_kv8_attn: AQ_MAX_M at most), 0 <= free_cap < 2^31.
+ * The plan keeps no count of a page's users: of requests that share pages each gives them back when it ends.  A caller that shares pages
+ * sets the length of such a request to 0 itself, and returns a page with its last user.
  * All or nothing: where the free pages, free_cap, table_width or n_rows do not suffice, or a length is negative, lengths, tables and free pages
  * stay as they were, the step has no rows (row_start 0, pos -1), and aq_check returns AQ_ERR_RANGE.
  */
@@ -266,9 +270,10 @@ aq_status_t aq_kv8_append(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* bat
  *   scratch_dev : DEVICE, 256-byte aligned, AQ_KV8_SCRATCH_BYTES, ZERO before its first use; a call leaves it as the next one wants it.
  *             Calls that may overlap in time (streams, captured graphs) need scratch of their own.
  * Built for decode (a few new tokens per request against long contexts); more rows per request are right but re-read the cache
- * for every 8 (head_dim 256) or 16 of a head's query rows.  A query row enters the products in 16 bits against its largest magnitude (off by
- * 2^-16 of it at most; bfloat16 rows under 2^-113: by 2^-128), the products with the codes are exact, weights enter the second product in 16 bits against the largest of their 32
- * positions (off by 2^-17 of that) and are summed as rounded, sums over positions are binary32: against the exact result for the
+ * for every 8 (head_dim 256) or 16 of a head's query rows.  Two roundings go beyond binary32's: a query row enters the products in 16 bits
+ * against its largest magnitude (an element is off by 1/65278 of that at most; bfloat16 rows under 2^-113: by 2^-128), so elements far under the
+ * largest keep fewer bits than they came with; and weights enter the second product in 16 bits against the largest of their 32 positions (off by
+ * 1/131070 of that, so a lighter one becomes 0).  The products with the codes are exact, the weights are summed as rounded, sums over positions are binary32: against the exact result for the
  * cached values an output is off by at most about 2^-12 (sum_p softmax_p |V[p]| + what that sum would be with every |V[p]| at its block's
  * largest), the scores' part and its own rounding.  bfloat16 values: the sum of their magnitudes over the positions has to fit binary32, and the absolute
  * error grows by 2^-122 for every 32 positions.  A query row with a NaN or an infinity gives NaN.
@@ -287,7 +292,8 @@ aq_status_t aq_kv8_attn(const aq_kv8_cache_t* cache, const aq_kv8_batch_t* batch
  *   AQ_ROPE_NONE    f_i as it is                AQ_ROPE_LINEAR  f_i / factor
  *   AQ_ROPE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in theta's place (rot_dim = 2: as it is)
  *   AQ_ROPE_PARTS   r = trained * f_i / (2 pi) rotations over the trained length: f_i for r >= high, f_i / factor for r <= low, in between
- *                   mixed in proportion; low, high 0: 1 and 32
+ *                   mixed in proportion to r; low, high 0: 1 and 32.  (A model whose ramp runs over the pairs' numbers instead, between
+ *                   ends rounded to whole pairs, has other frequencies: set aq_rope_t.turns to them after the call.)
  * magnitude: what rotated values are multiplied by; 0: 0.1 ln(factor) + 1 for AQ_ROPE_PARTS, else 1.
  *   layout: AQ_ROPE_HALF pairs (i, i + rot_dim / 2), AQ_ROPE_PAIRS pairs (2 i, 2 i + 1).  theta > 1, factor >= 1, trained >= 1 (AQ_ROPE_PARTS).
  */

@@ -190,8 +190,8 @@ constexpr int KW_WARPS = 4, KW_CTAS = 6;
 __device__ __forceinline__ float kw_up11(float x) { return __uint_as_float(kv8_up11(__float_as_uint(x))); }
 __device__ __forceinline__ float kw_up11_normal(float x) { return __uint_as_float((__float_as_uint(x) + 0x1FFFu) & ~0x1FFFu); }   // (of a subnormal: more)
 
-// rint(x / s) for |x / s| < 2^21 as the low bits of a float: the quotient correctly rounded (x inv, corrected by its exact remainder),
-// then rounded to a whole number by adding 1.5 * 2^23.  inv = 1 / s rounded; s in 2^-60 .. 2^125.
+// rint(x / s) for |x / s| < 2^21 as the low bits of a float: the quotient correctly rounded (x inv, corrected by its exact remainder: P. Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), then rounded to a whole number by adding 1.5 * 2^23.  inv = 1 / s rounded; s in 2^-60 .. 2^125.
 __device__ __forceinline__ uint32_t kw_quotient(float x, float s, float inv) {
     const float q = x * inv;
     return __float_as_uint(fmaf(fmaf(-q, s, x), inv, q) + 12582912.f);

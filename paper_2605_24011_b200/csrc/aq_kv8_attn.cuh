@@ -6,14 +6,16 @@
 //
 // Why whole numbers.  The codes are signed bytes and so is what the tensor core multiplies (mma.sync.m16n8k32, 8-bit in, 32-bit sums,
 // as fast per instruction as its binary16 form with half the depth): keys go from the cache to the instruction as they are, values after
-// one byte permute per four codes; nothing is converted, and the sums are exact.  (With both made binary16 first, a tile of 128 dims took
+// one byte permute per four codes; no code is converted, and the sums of products are exact.  Queries and weights are rounded to 16 bits for
+// it, below.  (With both made binary16 first, a tile of 128 dims took
 // 706 instructions per warp; the kernel waited for its own arithmetic: 32 x 4096 positions x 8 heads 62.6 us, DRAM 48 % busy.)
 //   A tile is 32 positions, the span of one scale, so scales touch the sums and not the operands.  Positions (or dims) are the 16 rows
 //   of the instruction and its 8 columns are four query rows in two planes, high and low byte:
-//   q^ = rint(q 32639 / max|q|) = 256 hi + lo, off by at most 2^-16 of the row's largest magnitude (a binary16 or bfloat16 q is
-//       itself known to 2^-12 or 2^-9 of each element).  hi and lo sums of a query lie in one lane: S = 256 hi + lo.
+//   q^ = rint(q 32639 / max|q|) = 256 hi + lo, off by at most 1/65278 of the row's largest magnitude (a binary16 or bfloat16 q is
+//       itself known to 2^-11 or 2^-8 of each element: one under 1/32 of the largest keeps less than binary16 had, under 1/256 than bfloat16).
+//       hi and lo sums of a query lie in one lane: S = 256 hi + lo.
 //   P = rint(65535 exp2(S - the tile's largest S)): 16 bits against the tile's own largest weight, so a tile loses what lies under
-//       2^-17 of that and no tile is lost for being light.  Transposed by movmatrix and split into byte planes by a permute.  sum(P) is a
+//       1/131070 of that and no tile is lost for being light.  Transposed by movmatrix and split into byte planes by a permute.  sum(P) is a
 //       product with ones: the normaliser sums what the values are weighted with.
 //   O = al O + 2^-16 vs fac (256 hi + lo) in binary32 (2^-16: the sum of weighted values fits where the values' own sum does); ldmatrix.trans on pairs of bytes gives dims 2g, 2g + 1 of two positions per register.
 // A NaN (of a scale, of a query row) travels in the scales: F, fac.
@@ -21,10 +23,10 @@
 // warp; runs differ by one place at most whatever the requests' lengths are.  What a warp finishes alone it writes; pieces of an item are merged
 // over the warps of the CTA in shared memory, then over the CTAs in the scratch by the last CTA to arrive (counters; nobody waits), in two
 // levels above 14 CTAs.  All sums go in a fixed order.  Where items are short, or all alike, a CTA's share is of whole ones.
-// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 46.7 us, 5.75 TB/s, 0.88 of the copy rate (from the L2 instead of
+// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 46.5 us, 5.78 TB/s, 0.88 of the copy rate (from the L2 instead of
 // HBM it takes 32.8: what remains is the start, the unequal speed of the SMs and the merge in the CTA); one request of 512 positions, 32 heads:
-// 7.2 us; 100001 positions, 8 heads of 256 on 1: 24.6 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows):
-// 63.5 us for 296 MB (57.9 from the L2: bound by the arithmetic, 840 instructions a tile at 46 % of the issue slots).
+// 7.35 us; 100001 positions, 8 heads of 256 on 1: 24.4 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows):
+// 63.4 us for 296 MB (57.9 from the L2: held up by the arithmetic, 840 instructions a tile at 46 % of the issue slots).
 // Fewer warps are slower where the arithmetic counts (61 ragged requests: 66.3 us with 8), more do not fit the registers (168 each
 // with 12: with the walks' state in them 148 us).
 // (Included by aq_kv8.cu alone, which has the status word and the host calls.)
@@ -921,7 +923,8 @@ cudaError_t launch_kv8_attn(const aq_kv8_cache_t& c, const aq_kv8_batch_t& b, co
     a.tickets = reinterpret_cast<unsigned*>(sc);
     a.part = sc + KA_TICKET_BYTES;
     // query rows per pass over a request's keys and values: what it has of them; where requests may differ, half as many again as on average
-    // (slots without rows and requests with fewer lie in the average; a second pass over a long request costs more than empty columns)
+    // (slots without rows and requests with fewer lie in the average; a second pass over a long request costs more than empty columns).  The
+    // host knows the step's rows and not whose they are: rows of nobody count, and a prompt among decodes does.
     const int64_t each = b.row_start_dev ? (T <= a.B ? 1 : ((int64_t)3 * T + a.B) / (2 * (int64_t)a.B)) : a.n_each;
     const int64_t rows = a.G * each;
     const int qt = rows <= 4 ? 1 : rows <= 8 || c.head_dim == 256 ? 2 : rows <= 12 ? 3 : 4;

@@ -1,6 +1,6 @@
 // Python calls of the batch-serving operators straight from torch tensors: checks of the arguments and marshalling only, the work is
-// libaq's (include/aq.h).  A decode step makes three of these calls per layer; through ctypes one cost the host 7.5 to 9.6 us, most of it
-// in asking tensors for their properties from Python and in converting up to fifteen arguments.
+// libaq's (include/aq.h).  A decode step makes three of these calls per layer; through ctypes one cost the host 6.3 to 9.5 us (here 2.6 to
+// 3.5), most of it in asking tensors for their properties from Python and in converting up to fifteen arguments.
 #include <Python.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
