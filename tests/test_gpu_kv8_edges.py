@@ -141,3 +141,37 @@ def test_attention_few_items_and_one_long_one(aq, D, G):
     """Fewer items than CTAs, one far longer than the average: shared by CTAs while the others stay short."""
     _check_attn(aq, [600 * 32] + [29 * 32] * 39, 1, G, D, 128, seed=98, outs=("f32",))
     _check_attn(aq, [9, 60 * 32, 40, 64], 2, G, D, 32, rows=[1, 2, 1, 0], seed=99, outs=("f32",))
+
+
+@pytest.mark.parametrize("name,big", (("f16", 100.0), ("f16", 3000.0), ("bf16", 100.0), ("bf16", 30000.0)))
+@pytest.mark.parametrize("D,G", ((64, 1), (128, 4), (256, 8)))
+def test_attention_of_queries_with_outliers(aq, D, G, name, big):
+    """A few elements far larger than the rest, on channels where the keys are small: the module's tolerance, 1.03 times
+    it as a query's element is off by 1/65278 of its row's largest, 1.004 2^-16, where it counts 2^-16."""
+    s = Served(aq, [700, 90], 2, D, 64, 100)
+    for channel in (3, D - 5):
+        s.k[..., channel] = torch.sign(s.k[..., channel]).to(torch.int8)
+    s.cache = aq.Kv8Cache(s.k.cuda(), s.v.cuda(), s.ks.cuda(), s.vs.cuda())
+    q = torch.randn(2, 2 * G, D, generator=torch.Generator().manual_seed(100))
+    q[..., 3], q[..., D - 5] = big, -0.8 * big
+    q = q.to({"f16": torch.float16, "bf16": torch.bfloat16}[name])
+    want, tol = _attn_reference(s, q.double().numpy(), [1, 1], 0.0)
+    for out_type, half in ((torch.float32, 2.0 ** -24), (q.dtype, 2.0 ** -11 if name == "f16" else 2.0 ** -8)):
+        out = torch.empty(2, 2 * G, D, dtype=out_type, device="cuda")
+        aq.aq_kv8_attn(s.cache, s.batch(aq), q.cuda(), out, aq.aq_kv8_scratch())
+        aq.aq_check()
+        assert np.all(np.abs(out.double().cpu().numpy() - want) <= 1.03 * tol + half * (np.abs(want) + tol) + (2.0 ** -25 if name == "f16" else 0))
+
+
+@pytest.mark.parametrize("layout", ("half", "pairs"))
+def test_rope_rows_of_frequencies_set_by_the_caller(aq, layout):
+    rope = aq.aq_rope_setup(64, layout=layout)
+    f = np.random.default_rng(101).random(32) * 0.7
+    for i, w in enumerate(f):
+        rope.turns[i] = w / (2 * np.pi)
+    x = torch.randn(9, 3, 80, generator=torch.Generator().manual_seed(101))
+    pos = [0, 1, 17, 5000, -1, 99, 3, 2, 700]
+    got = aq.aq_rope_rows(rope, x.cuda(), _i32(pos)).double().cpu().numpy()
+    want = O.rope_rows(x.double().numpy(), pos, f, layout)
+    # as in test_gpu_kv8.py; the angle's two roundings in binary64 are under 2^-38 radians at 5000
+    assert np.all(np.abs(got - want) <= 2.0 ** -21 * 2 * np.abs(x.numpy()).max() + 2.0 ** -24 * np.abs(want))
