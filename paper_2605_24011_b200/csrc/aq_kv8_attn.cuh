@@ -23,10 +23,10 @@
 // warp; runs differ by one place at most whatever the requests' lengths are.  What a warp finishes alone it writes; pieces of an item are merged
 // over the warps of the CTA in shared memory, then over the CTAs in the scratch by the last CTA to arrive (counters; nobody waits), in two
 // levels above 14 CTAs.  All sums go in a fixed order.  Where items are short, or all alike, a CTA's share is of whole ones.
-// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 46.5 us, 5.78 TB/s, 0.88 of the copy rate (from the L2 instead of
+// Measured: 32 requests x 4096 positions, 32 heads on 8 of 128, binary16: 46.7 us, 5.75 TB/s, 0.88 of the copy rate (from the L2 instead of
 // HBM it takes 32.8: what remains is the start, the unequal speed of the SMs and the merge in the CTA); one request of 512 positions, 32 heads:
-// 7.35 us; 100001 positions, 8 heads of 256 on 1: 24.4 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows):
-// 63.4 us for 296 MB (57.9 from the L2: held up by the arithmetic, 840 instructions a tile at 46 % of the issue slots).
+// 7.2 us; 100001 positions, 8 heads of 256 on 1: 24.4 us, ten of them merging 148 CTAs' parts; 61 ragged requests of 3 tokens (12 query rows):
+// 63.8 us for 296 MB (57.9 from the L2: held up by the arithmetic, 840 instructions a tile at 46 % of the issue slots).
 // Fewer warps are slower where the arithmetic counts (61 ragged requests: 66.3 us with 8), more do not fit the registers (168 each
 // with 12: with the walks' state in them 148 us).
 // (Included by aq_kv8.cu alone, which has the status word and the host calls.)
@@ -150,7 +150,7 @@ __device__ __forceinline__ KaSeq ka_seq(const KaArgs& a, int b, int rows) {
     s.row0 = r.first;
     s.n = r.n;
     s.L = max(a.lens[b], 0);   // (rows' positions follow from it, as the append has them, whether they fit or not)
-    const int held = (int)min((int64_t)s.L, a.width << (a.shift + 5));
+    const int held = min(s.L, (int)a.width << (a.shift + 5));   // (2^30 at most)
     s.nt = max(1, (held + KA_TILE - 1) / KA_TILE);   // (a request without positions has one tile that is not read: its rows become 0)
     s.rb = (s.n * a.G + rows - 1) / rows;   // (n G <= 2^20)
     return s;
